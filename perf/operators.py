@@ -4,10 +4,10 @@ elementary torch operations, and the call that a serving program makes.
 The cache (K and V apart, head-major pages): e4m3 codes and one exponent byte
 E = e + 127 for each (page, KV head, block of tokens); a stored element is
 code * 2^e, e the least exponent (at least -126) with
-amax(block) <= 448 * 2^e.  Byte order of the codes of 16 tokens of a head:
-  K  [d / 64][dim / 16 % 4][token][dim % 16]
-  V  [d / 64][token / 4][dim / 4 % 16][dim % 4][token % 4]
-in pools [pages][KV heads][P / 16] of those, exponents [pages][KV heads][P / block].
+amax(block) <= 448 * 2^e.  Codes:
+  K  [pages][KV heads][P][d]
+  V  [pages][KV heads][P / 16][d / 64][token / 4 % 4][dim / 4 % 16][dim % 4][token % 4]
+and exponents [pages][KV heads][P / block].
 
 Keys of a case:
   op        append   rows of K and V into their pages, one or many requests
@@ -297,25 +297,26 @@ def run(s):
 
 # ---------------------------------------------------------------- the plain forms
 def _code_view(codes, case, half):
-    """The codes as [page][head][tile] and the orders given above."""
-    lead = (-1, case["hkv"], PAGE // 16, case["d"] // 64)
-    return codes.view(*lead, 4, 16, 16) if half == 0 else codes.view(*lead, 4, 16, 4, 4)
+    """The codes as [page][head] and the orders given above."""
+    if half == 0:
+        return codes.view(-1, case["hkv"], PAGE, case["d"])
+    return codes.view(-1, case["hkv"], PAGE // 16, case["d"] // 64, 4, 16, 4, 4)
 
 
 def _put(codes, case, half, page, pos, x):
     """Codes x [rows][heads][d] to their places."""
-    t, c, chunks = pos % PAGE, _code_view(codes, case, half), case["d"] // 64
+    t, c = pos % PAGE, _code_view(codes, case, half)
     if half == 0:
-        c[page, :, t // 16, :, :, t % 16] = x.view(-1, case["hkv"], chunks, 4, 16)
+        c[page, :, t] = x
     else:
-        c[page, :, t // 16, :, t % 16 // 4, :, :, t % 4] = x.view(-1, case["hkv"], chunks, 16, 4)
+        c[page, :, t // 16, :, t % 16 // 4, :, :, t % 4] = x.view(-1, case["hkv"], case["d"] // 64, 16, 4)
 
 
 def _get(codes, case, half, page, pos):
     """Codes [rows][heads][d] of places."""
     t, c = pos % PAGE, _code_view(codes, case, half)
     if half == 0:
-        x = c[page, :, t // 16, :, :, t % 16]
+        x = c[page, :, t]
     else:
         x = c[page, :, t // 16, :, t % 16 // 4, :, :, t % 4]
     return x.reshape(-1, case["hkv"], case["d"])
@@ -380,10 +381,10 @@ def _cached(s, half):
     case, (codes, exps) = s["case"], s["pool"][half:half + 2]
     hkv, d = case["hkv"], case["d"]
     pages = s["tables"].clamp_min(0).long()
-    c = _code_view(codes, case, half)[pages]  # [batch][page][head][tile][d / 64]...
-    if half == 0:  # ...[dim / 16][token][dim]
-        c = c.permute(0, 2, 1, 3, 6, 4, 5, 7)
-    else:          # ...[token / 4][dim / 4][dim][token]
+    c = _code_view(codes, case, half)[pages]  # [batch][page][head]...
+    if half == 0:  # ...[token][dim]
+        c = c.transpose(1, 2)
+    else:          # ...[tile][d / 64][token / 4][dim / 4][dim][token]
         c = c.permute(0, 2, 1, 3, 5, 8, 4, 6, 7)
     x = c.reshape(pages.shape[0], hkv, -1, d).view(torch.float8_e4m3fn).float()
     e = exps.view(-1, hkv, PAGE // case["block"])[pages].transpose(1, 2).int() - 127
@@ -549,10 +550,10 @@ def _exact_pool(case, pages, half):
 
 def _exact_order(x, case, half):
     """Rows [page, head, slot][d] in the order in which the pool holds them."""
-    lead = (-1, PAGE // 16)
     if half == 0:
-        return x.view(*lead, 16, case["d"] // 64, 4, 16).permute(0, 1, 3, 4, 2, 5).reshape(-1)
-    return x.view(*lead, 4, 4, case["d"] // 64, 16, 4).permute(0, 1, 4, 2, 5, 6, 3).reshape(-1)
+        return x.reshape(-1)
+    x = x.view(-1, PAGE // 16, 4, 4, case["d"] // 64, 16, 4)
+    return x.permute(0, 1, 4, 2, 5, 6, 3).reshape(-1)
 
 
 def exact(case, seed):
