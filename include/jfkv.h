@@ -575,6 +575,166 @@ jf_status jf_tq4_reconstruct(const jf_kv_layout* layout, const void* k_words,
                              int32_t n_pos, int32_t kv0, int32_t num_heads,
                              void* k_out, void* v_out, hipStream_t stream);
 
+/* ---------------------------------------------------------------- KV8
+ * An 8-bit cache beside the 4-bit ones, for models that do not bear 4 bits,
+ * and what shortens a cache: the attention weights that its positions receive,
+ * and eviction by them.  Query heads share KV heads and requests own page
+ * tables as everywhere in this library.
+ *
+ * Stored element: c * 2^e, c an e4m3 code (OCP: 4 exponent and 3 mantissa
+ * bits, largest 448, no infinity), e one exponent for each (page, KV head,
+ * block of group_size consecutive positions), the same for K and V apart.
+ * jf_kv_layout.group_size counts POSITIONS here: 16, 32, 64 or 128, a divisor of
+ * page_size.  head_dim is 64, 128 or 256, page_size a multiple of 64 up to 4096.
+ * Pool (jf_kv_pool_ptrs; codes 16-byte aligned, k_meta and v_meta hold the
+ * exponent bytes):
+ *   k_codes  uint8 [NP][Hkv][P][d]
+ *   v_codes  uint8 [NP][Hkv][P/16][d/64][4][16][4][4]: token t, dim c of a
+ *            page's head lie at [t/16][c/64][t%16/4][c%64/4][c%4][t%4]
+ *   k_meta, v_meta  uint8 [NP][Hkv][P/group_size]  e + 127
+ * Quantizer (bit-exact contract), per block: amax over the finite elements of
+ * the rows; e = the least exponent >= -126 with amax <= 448 * 2^e (a block of
+ * zeros: -126); c = x * 2^-e rounded to the nearest e4m3 value, ties to even.
+ * Inputs must be finite; an infinity is stored as the block's largest value
+ * (+-448 * 2^e) and a NaN as +0, so that no stored code is a NaN.
+ *
+ * Types: k_new, v_new, q and out are fp16 (JF_F16) or bf16 (JF_BF16), one type
+ * per call; products run on the matrix cores with fp32 accumulation, codes
+ * enter them exactly, softmax statistics and sums are fp32.  Every function
+ * returns JF_ERR_UNSUPPORTED for a geometry, type or size that is not
+ * implemented and JF_ERR_INVALID for NULL or misaligned pointers, bad sizes, a
+ * short workspace or a non-finite scale; nothing is launched then. */
+typedef enum { JF_F16 = 0, JF_BF16 = 1 } jf_dtype;
+
+/* Bytes of one codes array and of one exponent array (the same for K and V). */
+jf_status jf_kv8_pool_bytes(const jf_kv_layout* layout, size_t* codes_bytes,
+                            size_t* exps_bytes);
+
+/* Quantize rows of K and V into their pages.  k_new, v_new: [total_tok][Hkv][d]
+ * (device, 16-byte aligned); cu_tok, start_pos, block_tables, B, max_pages as in
+ * jf_kv_quantize_append: rows whose position is negative or beyond the table, or
+ * whose page ID is outside [0, num_pages), are skipped.
+ * A block that holds positions before request b's first new row (start_pos[b]
+ * inside a block) keeps them: its exponent becomes the larger of the stored one
+ * and the new rows' one, and if that raises it, the stored codes of those earlier
+ * positions are rescaled (exact but for codes that become subnormal, which are
+ * rounded once more).  Slots behind the last new row are left as they are.
+ * Rows of one call must not share a position; pages must not be shared. */
+jf_status jf_kv8_append(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
+                        int32_t dtype, const void* k_new, const void* v_new,
+                        const int32_t* cu_tok, const int32_t* start_pos,
+                        const int32_t* block_tables, int32_t B, int32_t max_pages,
+                        int32_t total_tok, hipStream_t stream);
+
+/* Decode attention: the last num_queries (1..4) positions of request b, already
+ * appended, are its query tokens; token k sees the positions 0 .. seq_lens[b] -
+ * num_queries + k.  Lengths are cut to the table's capacity; a token that sees
+ * nothing gets a zero row.
+ *   q, out      [B][num_queries][num_q_heads][d] (device, 16-byte aligned)
+ *   max_splits  cap on partials per request and KV head (1..1024).  A request's
+ *               output depends on neither the batch nor the other requests.
+ *   workspace   16-byte aligned device scratch of at least
+ *               jf_kv8_decode_workspace_bytes().  Its first 262,144 bytes must be
+ *               zero before the first call; every call that completes leaves them
+ *               zero (the workspace of jf_decode_attn_q4 has the same rule, and
+ *               one that is large enough serves both).  Calls that may overlap in
+ *               time, replays of graphs among them, must not share one.
+ *   weights     NULL, or fp32 (device): weights[(b * Hkv + kv) * weights_stride
+ *               + t] grows by the sum, over the call's tokens and the query heads
+ *               of kv, of the attention weight of position t < seq_lens[b].
+ *               Entries from seq_lens[b] on are left as they are.
+ *               weights_stride >= max_pages * page_size; the workspace is then
+ *               sized with weight_pages = max_pages (else 0), 4 bytes per score.
+ * Positions on a page ID outside [0, num_pages) do not contribute.
+ * B <= 65,535 and B * num_q_heads * num_queries <= 65,536. */
+jf_status jf_kv8_decode_workspace_bytes(const jf_kv_layout* layout, int32_t B,
+                                        int32_t num_queries, int32_t num_q_heads,
+                                        int32_t max_splits, int32_t weight_pages,
+                                        size_t* bytes);
+jf_status jf_kv8_decode_attn(const jf_kv_layout* layout,
+                             const jf_kv_pool_ptrs* pool, int32_t dtype,
+                             const void* q, int32_t B, int32_t num_queries,
+                             int32_t num_q_heads, const int32_t* block_tables,
+                             int32_t max_pages, const int32_t* seq_lens,
+                             float softmax_scale, int32_t max_splits,
+                             void* workspace, size_t workspace_bytes, void* out,
+                             float* weights, int64_t weights_stride,
+                             hipStream_t stream);
+
+/* Chunk attention of one request: rows 0 .. T-1 sit at positions prefix_len .. +
+ * T-1, which are already in the cache (append first, unlike jf_prefill_attn_q4),
+ * and attend causally to the positions 0 .. prefix_len + i, all read from the
+ * pages.
+ *   q, out     [T][num_q_heads][d] (device, 16-byte aligned)
+ *   lse        NULL, or fp32 [T][num_q_heads] (device): the natural logarithm of
+ *              the sum of exp(softmax_scale * q . k) over the positions seen
+ *              (-inf where there is none, for which out is zero)
+ *   workspace  NULL, or 16-byte aligned device scratch of at least
+ *              jf_kv8_prefill_workspace_bytes() (which may be 0): lets a chunk of
+ *              few rows share its keys among more blocks.  Its contents do not
+ *              matter.  Calls that may overlap in time must not share one.
+ *              Results with and without it are the same up to the order of sums.
+ * Positions on a page ID outside [0, num_pages) do not contribute. */
+jf_status jf_kv8_prefill_workspace_bytes(const jf_kv_layout* layout, int32_t T,
+                                         int32_t num_q_heads, int32_t prefix_len,
+                                         size_t* bytes);
+jf_status jf_kv8_prefill_attn(const jf_kv_layout* layout,
+                              const jf_kv_pool_ptrs* pool, int32_t dtype,
+                              const void* q, int32_t T, int32_t num_q_heads,
+                              const int32_t* block_table, int32_t max_pages,
+                              int32_t prefix_len, float softmax_scale,
+                              void* workspace, size_t workspace_bytes, void* out,
+                              float* lse, hipStream_t stream);
+
+/* Attention weights of a chunk's rows, added up per position: weights[kv *
+ * weights_stride + t] grows by the sum, over rows i and the query heads h of kv
+ * with t <= prefix_len + i, of exp(softmax_scale * q_ih . k_t - lse_ih).  q and lse
+ * as of jf_kv8_prefill_attn; for the last rows of a chunk only (an observation
+ * window) pass their q, lse and prefix_len.  Entries from prefix_len + T on, and
+ * those of positions on a page ID outside [0, num_pages), are left as they are.
+ * weights: fp32 (device), weights_stride >= prefix_len + T.  The sums' order is
+ * fixed: the same inputs give the same bits. */
+jf_status jf_kv8_attn_weights(const jf_kv_layout* layout,
+                              const jf_kv_pool_ptrs* pool, int32_t dtype,
+                              const void* q, const float* lse, int32_t T,
+                              int32_t num_q_heads, const int32_t* block_table,
+                              int32_t max_pages, int32_t prefix_len,
+                              float softmax_scale, float* weights,
+                              int64_t weights_stride, hipStream_t stream);
+
+/* Eviction by accumulated weight.  For each request b and KV head, m =
+ * min(seq_lens[b], keep) positions stay: the last min(recent, seq_lens[b]) and,
+ * of the others, those of the largest weights (ties: the lowest positions; a NaN
+ * counts as larger than any number).  They are moved, in their order, to the
+ * positions 0 .. m - 1 of dst_tables' pages, whose blocks get exponents of their
+ * own (a moved code changes by a power of two; exact but for codes that become
+ * subnormal).  The caller goes on with dst_tables and length m, and returns the
+ * old pages.
+ *   weights       fp32 [B][Hkv][weights_stride] (device), as added up by the
+ *                 calls above; weights_stride >= max_pages * page_size
+ *   keep, recent  keep >= 1, 0 <= recent <= keep
+ *   dst_tables    int32 [B][dst_max_pages] (device), keep <= dst_max_pages *
+ *                 page_size; its pages must be none of the source pages, and
+ *                 distinct.  Positions on a page ID outside [0, num_pages) are not
+ *                 written (source: they are moved as zeros).
+ *   workspace     16-byte aligned device scratch of at least
+ *                 jf_kv8_evict_workspace_bytes() (may be 0, then NULL will do);
+ *                 its contents do not matter.  Calls that may overlap in time
+ *                 must not share one.
+ *   kept          int32 [B][Hkv][keep]: the positions that stay, ascending, then -1
+ *   kept_weights  fp32 [B][Hkv][keep]: their weights, then 0
+ * Slots behind position m - 1 are left as they are. */
+jf_status jf_kv8_evict_workspace_bytes(const jf_kv_layout* layout, int32_t B,
+                                       int32_t max_pages, int32_t keep,
+                                       size_t* bytes);
+jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
+                       int32_t B, const int32_t* block_tables, int32_t max_pages,
+                       const int32_t* seq_lens, const float* weights,
+                       int64_t weights_stride, int32_t keep, int32_t recent,
+                       const int32_t* dst_tables, int32_t dst_max_pages,
+                       void* workspace, size_t workspace_bytes, int32_t* kept,
+                       float* kept_weights, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,7 +20,8 @@ LIB = os.path.join(HERE, "libjfkv.so")
 ARCH = os.environ.get("JFKV_ARCH", "gfx950")
 
 SOURCES = ["jfkv_host.cpp", "quantize.hip", "decode.hip", "prefill.hip", "tq4.hip",
-           "tq4_decode.hip", "reconstruct.hip", "pages.hip", "calib.hip"]
+           "tq4_decode.hip", "reconstruct.hip", "pages.hip", "calib.hip", "kv8_host.cpp",
+           "kv8_append.hip", "kv8_decode.hip", "kv8_prefill.hip", "kv8_evict.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
@@ -28,8 +29,10 @@ DEVICE = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-p
           "-munsafe-fp-atomics"]
 # Per-source device flags.  decode.hip: matrix-core results stay in ordinary
 # VGPRs (its rare rescale multiplies them on the VALU; with accumulation
-# registers the compiler copies them out and back around every row).
-EXTRA = {"decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+# registers the compiler copies them out and back around every row); the
+# decode over the 8-bit cache likewise.
+EXTRA = {"decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "kv8_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:

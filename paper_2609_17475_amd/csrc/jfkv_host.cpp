@@ -25,8 +25,10 @@
 #include "jfkv_prefill_plan.h"
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
+
+namespace jfkv {
 
 jf_status fail(jf_status st, const char* fmt, ...) {
   char buf[512];
@@ -47,6 +49,14 @@ jf_status device_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return ok();
   return fail(JF_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace jfkv
+
+namespace {
+
+using jfkv::device_status;
+using jfkv::fail;
+using jfkv::ok;
 
 jf_status check_layout(const jf_kv_layout* L) {
   if (!L) return fail(JF_ERR_INVALID, "layout is NULL");

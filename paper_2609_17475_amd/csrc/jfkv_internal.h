@@ -10,6 +10,12 @@
 
 namespace jfkv {
 
+// Error reporting of the C entry points: fail() keeps the message for
+// jf_last_error() and returns st, ok() clears it.
+jf_status fail(jf_status st, const char* fmt, ...);
+jf_status ok();
+jf_status device_status(hipError_t e, const char* what);
+
 // Decode workspace: a fixed region of uint32 completion counters (one per
 // request, KV head and head chunk; room for B * Hq <= kDecodeMaxHeads), then
 // the fp32 split records [B][Hq][max_splits][d + 4] (o/l, m, l; 16-byte
@@ -108,6 +114,59 @@ hipError_t launch_tq4_decode(const jf_kv_layout& L, const void* k_words, const v
                              int32_t B, int32_t Hq, const int32_t* block_tables,
                              int32_t max_pages, const int32_t* seq_lens, float softmax_scale,
                              int32_t max_splits, void* ws, void* out, hipStream_t stream);
+
+// ---- the 8-bit cache (jfkv_kv8.h)
+hipError_t launch_kv8_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                             const void* k_new, const void* v_new, const int32_t* cu_tok,
+                             const int32_t* start_pos, const int32_t* block_tables, int32_t B,
+                             int32_t max_pages, int32_t total_tok, hipStream_t stream);
+
+// Decode workspace: the completion counters and split records of the decode
+// over 4-bit pages (Hq * sq heads); where weights are added up, then the
+// log-sum-exps [B][Hkv][pairs] and the scores [B][Hkv][pairs][cap] of the call
+// (fp32; pairs = sq * Hq / Hkv, cap = positions of the tables, 0: none).
+struct Kv8Workspace {
+  size_t records, lse, logits, bytes;
+};
+inline Kv8Workspace kv8_workspace(int32_t B, int32_t sq, int32_t Hq, int32_t head_dim,
+                                  int32_t max_splits, int64_t cap) {
+  Kv8Workspace w;
+  w.records = kDecodeCounterBytes;
+  w.lse = decode_workspace_bytes(B, Hq * sq, head_dim, max_splits);
+  const size_t rows = (size_t)B * Hq * sq;
+  w.logits = w.lse + (cap ? (rows * sizeof(float) + 15) / 16 * 16 : 0);
+  w.bytes = w.logits + rows * (size_t)cap * sizeof(float);
+  return w;
+}
+// weights: nullptr, or fp32 [B][Hkv][stride] to which the call's are added.
+hipError_t launch_kv8_decode(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                             const void* q, int32_t B, int32_t sq, int32_t Hq,
+                             const int32_t* block_tables, int32_t max_pages,
+                             const int32_t* seq_lens, float softmax_scale, int32_t max_splits,
+                             void* ws, void* out, float* weights, int64_t stride,
+                             hipStream_t stream);
+
+// Chunk attention: splits of the keys (1: none), the bytes of their partials,
+// and the launch (ws used where splits > 1; lse may be nullptr).
+int kv8_prefill_splits(const jf_kv_layout& L, int32_t T, int32_t Hq, int32_t prefix_len);
+size_t kv8_prefill_bytes(const jf_kv_layout& L, int32_t T, int32_t Hq, int splits);
+hipError_t launch_kv8_prefill(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                              const void* q, int32_t T, int32_t Hq, const int32_t* block_table,
+                              int32_t prefix_len, float softmax_scale, int splits, void* ws,
+                              void* out, float* lse, hipStream_t stream);
+
+// The chunk's attention weights added to weights [Hkv][stride].
+hipError_t launch_kv8_weights(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                              const void* q, const float* lse, int32_t T, int32_t Hq,
+                              const int32_t* block_table, int32_t prefix_len, float softmax_scale,
+                              float* weights, int64_t stride, hipStream_t stream);
+
+// Eviction into the pages of dst_tables; kept, kept_w [B][Hkv][keep].
+hipError_t launch_kv8_evict(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, int32_t B,
+                            const int32_t* block_tables, int32_t max_pages,
+                            const int32_t* seq_lens, const float* weights, int64_t stride,
+                            int32_t keep, int32_t recent, const int32_t* dst_tables,
+                            int32_t dst_pages, int32_t* kept, float* kept_w, hipStream_t stream);
 
 // Read-rate calibration: one pass over bytes (a multiple of 16) of buf.
 hipError_t launch_read_stream(const void* buf, size_t bytes, int32_t blocks, uint32_t* sink,

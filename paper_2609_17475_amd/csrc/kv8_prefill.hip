@@ -1,0 +1,582 @@
+// Chunk attention over the 8-bit cache (format: jfkv_kv8.h): the T rows of a
+// chunk, already appended, attend causally to the prefix and to themselves,
+// all read from the pages; and the sums of such rows' attention weights.
+//
+//   s_it = scale * q_i . k_t  (t <= prefix + i),  lse_i = log sum_t exp(s_it)
+//   o_i = sum_t exp(s_it - lse_i) v_t,  w_t += sum_i exp(s_it - lse_i)
+//
+// Bound by the matrix cores and the vector work beside them (an exponential
+// and four more instructions per score, one conversion per two codes).  The
+// (row, head) pairs that read a KV head are the columns of the products, as in
+// kv8_decode.hip, whose operand layouts and exponents' handling are the same.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "jfkv_internal.h"
+#include "jfkv_kv8.h"
+
+namespace jfkv {
+namespace {
+
+using namespace kv8;
+
+constexpr int kTile = 64;        // positions of a tile (in one page)
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
+constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
+constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// Column sets of 16 per wave: two share every operand of K and V; at head_dim
+// 256 the accumulators of one fill the registers.
+template <int D>
+constexpr int col_sets() {
+  return D > 128 ? 1 : 2;
+}
+template <int D>
+constexpr int block_cols() {
+  return kWaves * 16 * col_sets<D>();
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float col_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float col_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// The query row of (row, head) as B operands: dims 64 c + 16 g + 8 j ..
+template <int C, bool BF16>
+__device__ __forceinline__ void load_q(u32x4 (&qf)[C][2], const uint16_t* qp, int g, uint32_t flip) {
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      qf[c][j] = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j) ^ flip;
+}
+
+// One block: block_cols columns of one KV head, the tiles of one split.  A tile's
+// K and V codes are fetched two tiles ahead into registers, go to LDS in
+// operand order one tile ahead (K: [16 positions][64 dims][lane][16 B]; V as it
+// lies), and are widened by each wave as it uses them.  SPLIT: fp32 partials
+// (o, m, l) to ws [split][Hkv][columns][D + 4] instead of rows.
+template <int D, bool BF16>
+__global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
+    const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
+    const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
+    const uint16_t* __restrict__ q, const int32_t* __restrict__ table, float* __restrict__ ws,
+    uint16_t* __restrict__ out, float* __restrict__ lse, int Hq, int Hkv, int P, int block_shift,
+    int num_pages, int T, int prefix, int n_rb, int n_split, float scale_log2, uint32_t flip) {
+  constexpr int C = D / 64, NC = col_sets<D>(), COLS = block_cols<D>();
+  constexpr int kItems = 128 * D / 16 / kThreads;  // 16-byte pieces of a tile per thread
+  __shared__ __align__(16) u32x4 tiles[2][8 * D];  // K, then V
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // KV head fastest (one XCD's L2 sees few heads), the longest row blocks first
+  const int kv = blockIdx.x % Hkv, rest = blockIdx.x / Hkv;
+  const int split = rest % n_split, rb = n_rb - 1 - rest / n_split;
+  const int gq = Hq / Hkv;
+  const int64_t ncols = (int64_t)T * gq, col_base = (int64_t)rb * COLS;
+  const int L = prefix + T;
+
+  const int row_hi = (int)((min(col_base + COLS, ncols) - 1) / gq);
+  const int64_t nt = (prefix + row_hi) / kTile + 1;
+  const int j0 = (int)(nt * split / n_split), j1 = (int)(nt * (split + 1) / n_split);
+
+  // the wave's columns
+  const int64_t wcol = col_base + wave * 16 * NC;
+  const bool active = wcol < ncols;
+  const int w_lo = active ? (int)(wcol / gq) : 0;  // its first and last row
+  const int w_hi = active ? (int)((min(wcol + 16 * NC, ncols) - 1) / gq) : -1;
+  int row[NC];
+  u32x4 qf[NC][C][2];
+#pragma unroll
+  for (int cs = 0; cs < NC; ++cs) {
+    const int64_t col = min(wcol + 16 * cs + n, ncols - 1);  // (columns past the end repeat the last)
+    row[cs] = (int)(col / gq);
+    load_q<C, BF16>(qf[cs], q + ((size_t)row[cs] * Hq + kv * gq + col % gq) * D, g, flip);
+  }
+
+  f32x4 acc[NC][C][4] = {};
+  float m[NC], l[NC];
+#pragma unroll
+  for (int cs = 0; cs < NC; ++cs) m[cs] = -INFINITY, l[cs] = 0.0f;
+  int e_ref = 0, e_top = -1000;
+
+  // ---- tile transport
+  u32x4 stage[kItems];
+  uint32_t exps_next = 0, exps = 0;  // lanes 0..3: K's exponent bytes of the tile, 4..7: V's
+  auto page_of = [&](int j) { return table[min(j, j1 - 1) * kTile / P]; };
+  auto fetch = [&](int j, int pid) {
+    const int slot0 = min(j, j1 - 1) * kTile % P;
+    const size_t run = (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv;
+    const uint8_t* kp = k_codes + (run * P + slot0) * D;
+    const uint8_t* vp = v_codes + (run * P + slot0) * D;
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int i = tid + k * kThreads;
+      if (i < 4 * D) {
+        const int r = i % D, ln = r & 63;
+        stage[k] = *reinterpret_cast<const u32x4*>(kp + ((i / D) * 16 + (ln & 15)) * D +
+                                                    (r >> 6) * 64 + (ln >> 4) * 16);
+      } else {
+        stage[k] = *reinterpret_cast<const u32x4*>(vp + (i - 4 * D) * 16);
+      }
+    }
+    const uint8_t* ep = (lane & 4) ? v_exps : k_exps;
+    exps_next = ep[run * (P >> block_shift) + ((slot0 + 16 * (lane & 3)) >> block_shift)];
+  };
+  auto deposit = [&](int j) {
+    if ((j + 1) * kTile > L) {
+      // slots not written yet: zeros for their values (their codes may be NaN)
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) {
+        const int i = tid + k * kThreads - 4 * D;
+        if (i >= 0) {
+          const int left = min(max(L - (j * kTile + (i / D) * 16 + (i % 64) / 16 * 4), 0), 4);
+          stage[k] &= left ? 0xffffffffu >> (8 * (4 - left)) : 0u;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) tiles[j & 1][tid + k * kThreads] = stage[k];
+  };
+
+  auto rescale = [&](int cs, float f) {
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= f;
+  };
+
+  auto compute = [&](int j) {
+    const u32x4* kt = tiles[j & 1];
+    const u32x4* vt = kt + 4 * D;
+    const int pos0 = j * kTile;
+    // scores, times f[t] in log2 units
+    f32x4 s[4][NC];
+    float f[4];
+    int ev[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int cs = 0; cs < NC; ++cs) s[t][cs] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const u32x4 kc = kt[t * D + c * 64 + lane];
+        const u32x4 a0 = widen8<BF16>(kc.x, kc.y), a1 = widen8<BF16>(kc.z, kc.w);
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a0, qf[cs][c][0], s[t][cs]);
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a1, qf[cs][c][1], s[t][cs]);
+      }
+      // (not 0, so that a hidden score times it stays -inf)
+      f[t] = fmaxf(scale_log2 * power2(__builtin_amdgcn_readlane((int)exps, t) - 127), 1e-37f);
+      ev[t] = __builtin_amdgcn_readlane((int)exps, 4 + t) - 127;
+    }
+    if (pos0 + kTile - 1 > prefix + w_lo) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (pos0 + 16 * t + 4 * g + i > prefix + row[cs]) s[t][cs][i] = -INFINITY;
+        if (pos0 + 16 * t >= L) f[t] = 1.0f, ev[t] = ev[0];  // (exponents not written yet)
+      }
+    }
+    // maxima
+    float top[NC];
+    bool raise = false;
+#pragma unroll
+    for (int cs = 0; cs < NC; ++cs) {
+      top[cs] = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        top[cs] = fmaxf(top[cs], f[t] * fmaxf(fmaxf(s[t][cs][0], s[t][cs][1]),
+                                              fmaxf(s[t][cs][2], s[t][cs][3])));
+      raise |= top[cs] > m[cs] + kMargin;
+    }
+    if (__any(raise)) {
+#pragma unroll
+      for (int cs = 0; cs < NC; ++cs) {
+        const float mn = fmaxf(m[cs], col_max(top[cs]));
+        const float by = m[cs] == -INFINITY ? 0.0f : exp2_(m[cs] - mn);
+        l[cs] *= by;
+        rescale(cs, by);
+        m[cs] = mn;
+      }
+    }
+    // the values' exponents: one reference for the tile, or one part per 16
+    // positions where they are too far apart for that
+    int lo = ev[0], hi = ev[0];
+#pragma unroll
+    for (int t = 1; t < 4; ++t) lo = min(lo, ev[t]), hi = max(hi, ev[t]);
+    const int parts = hi - lo <= kRefMax ? 1 : 4;
+    for (int part = 0; part < parts; ++part) {
+      if (parts > 1) lo = hi = part == 0 ? ev[0] : part == 1 ? ev[1] : part == 2 ? ev[2] : ev[3];
+      e_top = max(e_top, hi);
+      if (lo < e_ref || hi > e_ref + kRefMax) {
+        const int e = max(max(hi - kRefMax, lo - 4), e_top - kRefFloor);
+        const float by = __builtin_ldexpf(1.0f, e_ref - e);
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) rescale(cs, by);
+        e_ref = e;
+      }
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        u32x4 pf[NC];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int t = 2 * t2 + u;
+          const bool on = parts == 1 || part == t;
+          const float by = (float)(ev[t] - e_ref);
+#pragma unroll
+          for (int cs = 0; cs < NC; ++cs) {
+            const float mu = m[cs] == -INFINITY ? 0.0f : m[cs];
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = exp2_(fmaf(s[t][cs][i], f[t], by - mu));
+            if (on) {
+              if (ev[t] - e_ref >= -kRefMax) {
+                l[cs] = fmaf((p[0] + p[1]) + (p[2] + p[3]), power2(e_ref - ev[t]), l[cs]);
+              } else {  // (far below the largest values: P may vanish, l must not)
+                for (int i = 0; i < 4; ++i) l[cs] += exp2_(fmaf(s[t][cs][i], f[t], -mu));
+              }
+            }
+            pf[cs][2 * u] = on ? narrow2<false>(p[0], p[1]) : 0u;
+            pf[cs][2 * u + 1] = on ? narrow2<false>(p[2], p[3]) : 0u;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const u32x4 v0 = vt[2 * t2 * D + c * 64 + lane], v1 = vt[(2 * t2 + 1) * D + c * 64 + lane];
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) {
+            const u32x4 a = widen8<false>(v0[dt], v1[dt]);
+#pragma unroll
+            for (int cs = 0; cs < NC; ++cs) acc[cs][c][dt] = mma<false>(a, pf[cs], acc[cs][c][dt]);
+          }
+        }
+      }
+    }
+  };
+
+  if (j0 < j1) {
+    int pid = page_of(j0), pid1 = page_of(j0 + 1), pid2 = page_of(j0 + 2);
+    fetch(j0, pid);
+    exps = exps_next;
+    deposit(j0);
+    fetch(j0 + 1, pid1);
+    for (int j = j0; j < j1; ++j) {
+      __syncthreads();  // tile j is in LDS, tile j - 1 is done with
+      const uint32_t exps_1 = exps_next;
+      if (j + 1 < j1) deposit(j + 1);
+      fetch(j + 2, pid2);
+      const int pid3 = page_of(j + 3);
+      if (active && (uint32_t)pid < (uint32_t)num_pages && j * kTile <= prefix + w_hi) compute(j);
+      exps = exps_1;
+      pid = pid1, pid1 = pid2, pid2 = pid3;
+    }
+  }
+
+  // ---- rows out, or partials
+  if (!active) return;
+  const float unit = __builtin_ldexpf(1.0f, e_ref);
+#pragma unroll
+  for (int cs = 0; cs < NC; ++cs) {
+    const float den = col_sum(l[cs]);
+    const int64_t col = wcol + 16 * cs + n;
+    if (col >= ncols) continue;
+    if (n_split == 1) {
+      const float r = den > 0.0f ? unit / den : 0.0f;
+      const size_t at = (size_t)row[cs] * Hq + kv * gq + col % gq;
+      uint16_t* op = out + at * D + 16 * g;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          const f32x4(&a)[4] = acc[cs][c];
+          *reinterpret_cast<uint4*>(op + 64 * c + 4 * i) =
+              make_uint4(narrow2<BF16>(a[0][i] * r, a[1][i] * r),
+                         narrow2<BF16>(a[2][i] * r, a[3][i] * r),
+                         narrow2<BF16>(a[0][i + 1] * r, a[1][i + 1] * r),
+                         narrow2<BF16>(a[2][i + 1] * r, a[3][i + 1] * r));
+        }
+      if (lse && g == 0)
+        lse[at] = den > 0.0f ? (m[cs] + __log2f(den)) * (1.0f / kLog2e) : -INFINITY;
+    } else {
+      float* rec = ws + (((size_t)split * Hkv + kv) * ncols + col) * (D + 4);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(rec + 64 * c + 16 * g + 4 * i) =
+              f32x4{acc[cs][c][0][i], acc[cs][c][1][i], acc[cs][c][2][i], acc[cs][c][3][i]} * unit;
+      if (g == 0) rec[D] = m[cs], rec[D + 1] = den;
+    }
+  }
+}
+
+// Joins the splits' partials: a thread takes four dims of one column.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void kv8_prefill_combine_kernel(
+    const float* __restrict__ ws, uint16_t* __restrict__ out, float* __restrict__ lse, int Hq,
+    int Hkv, int64_t ncols, int n_split) {
+  const int gq = Hq / Hkv;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t at = i / (D / 4);  // (KV head, column)
+  const int d4 = (int)(i % (D / 4));
+  if (at >= ncols * Hkv) return;
+  float M = -INFINITY, den = 0.0f;
+  f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < n_split; ++s) {
+    const float* rec = ws + ((size_t)s * Hkv * ncols + at) * (D + 4);
+    const float ms = rec[D], mx = fmaxf(M, ms);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(rec + 4 * d4);
+    const float a = M == -INFINITY ? 0.0f : exp2_(M - mx), b = ms == -INFINITY ? 0.0f : exp2_(ms - mx);
+    num = num * a + o * b;
+    den = den * a + rec[D + 1] * b;
+    M = mx;
+  }
+  const float r = den > 0.0f ? 1.0f / den : 0.0f;
+  const int64_t kv = at / ncols, col = at % ncols;
+  const size_t dst = (size_t)(col / gq) * Hq + kv * gq + col % gq;
+  *reinterpret_cast<uint2*>(out + dst * D + 4 * d4) =
+      make_uint2(narrow2<BF16>(num.x * r, num.y * r), narrow2<BF16>(num.z * r, num.w * r));
+  if (lse && d4 == 0) lse[dst] = den > 0.0f ? (M + __log2f(den)) * (1.0f / kLog2e) : -INFINITY;
+}
+
+// ---- attention weights of a chunk's rows, added up per position
+//
+// A wave owns 16 NS positions, whose K it holds as matrix operands in
+// registers, and walks over all columns that see them; the columns' queries
+// (B operands) and (lse, row) pass through LDS, 64 columns at a time, shared
+// by the block's four waves.  No two waves add to the same position, so the
+// sums' order is fixed.  Weights are never rounded below fp32.
+constexpr int kWWaves = 4;
+constexpr int kWThreads = 64 * kWWaves;
+constexpr int kWCols = 64;
+
+template <int D, bool BF16, int NS>
+__global__ __launch_bounds__(kWThreads) void kv8_weights_kernel(
+    const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
+    const uint16_t* __restrict__ q, const float* __restrict__ lse,
+    const int32_t* __restrict__ table, float* __restrict__ weights, int64_t stride, int Hq, int Hkv,
+    int P, int block_shift, int num_pages, int T, int prefix, float scale_log2) {
+  constexpr int C = D / 64;
+  constexpr int kItems = kWCols * D * 2 / 16 / kWThreads;
+  __shared__ __align__(16) u32x4 qs[2][kWCols * D / 8];  // [16 columns][c][j][lane]
+  __shared__ float s_lse[2][kWCols];
+  __shared__ int s_row[2][kWCols];
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kv = blockIdx.x % Hkv, gq = Hq / Hkv;
+  const int64_t ncols = (int64_t)T * gq;
+  const int L = prefix + T;
+  const int64_t base = (int64_t)(blockIdx.x / Hkv) * (kWWaves * 16 * NS);
+  const int64_t key0_64 = base + wave * 16 * NS;
+  const bool mine = key0_64 < L;
+  const int key0 = mine ? (int)key0_64 : 0;
+
+  // the wave's keys as A operands, and their factors
+  const int pid = table[key0 / P];
+  const bool on = mine && (uint32_t)pid < (uint32_t)num_pages;
+  const size_t run = (size_t)(on ? pid : 0) * Hkv + kv;
+  const int slot0 = key0 % P;
+  u32x4 kf[NS][C][2];
+  float f[NS];
+#pragma unroll
+  for (int t = 0; t < NS; ++t) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const u32x4 kc = *reinterpret_cast<const u32x4*>(k_codes + (run * P + slot0 + 16 * t + n) * D +
+                                                       64 * c + 16 * g);
+      kf[t][c][0] = widen8<BF16>(kc.x, kc.y), kf[t][c][1] = widen8<BF16>(kc.z, kc.w);
+    }
+    f[t] = scale_log2 * power2((int)k_exps[run * (P >> block_shift) + ((slot0 + 16 * t) >> block_shift)] - 127);
+  }
+  float w[NS][4] = {};
+
+  // columns from the first row that sees the block's first key
+  const int64_t col0 = max((int64_t)0, base - prefix) * gq / kWCols * kWCols;
+  u32x4 stage[kItems];
+  float stage_lse = 0.0f;
+  int stage_row = 0;
+  auto fetch = [&](int64_t at) {
+#pragma unroll
+    for (int k = 0; k < kItems; ++k) {
+      const int i = tid + k * kWThreads;  // [16 columns][c][j][lane]
+      const int ln = i & 63, cj = (i >> 6) % (2 * C), grp = (i >> 6) / (2 * C);
+      const int64_t col = min(at + 16 * grp + (ln & 15), ncols - 1);
+      stage[k] = *reinterpret_cast<const u32x4*>(q + ((size_t)(col / gq) * Hq + kv * gq + col % gq) * D +
+                                                 64 * (cj >> 1) + 16 * (ln >> 4) + 8 * (cj & 1));
+    }
+    if (tid < kWCols) {
+      const int64_t col = at + tid, cc = min(col, ncols - 1);
+      stage_row = (int)(cc / gq);
+      const float z = lse[(size_t)stage_row * Hq + kv * gq + cc % gq];
+      // a row that sees nothing, and columns past the end, weigh nothing
+      stage_lse = col < ncols && z != -INFINITY ? z * kLog2e : INFINITY;
+    }
+  };
+  if (col0 < ncols) {
+    fetch(col0);
+    int buf = 0;
+    for (int64_t at = col0; at < ncols; at += kWCols, buf ^= 1) {
+#pragma unroll
+      for (int k = 0; k < kItems; ++k) qs[buf][tid + k * kWThreads] = stage[k];
+      if (tid < kWCols) s_lse[buf][tid] = stage_lse, s_row[buf][tid] = stage_row;
+      __syncthreads();
+      if (at + kWCols < ncols) fetch(at + kWCols);
+      if (on) {
+#pragma unroll
+        for (int grp = 0; grp < kWCols / 16; ++grp) {
+          f32x4 s[NS];
+#pragma unroll
+          for (int t = 0; t < NS; ++t) s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const u32x4 b = qs[buf][((grp * C + c) * 2 + j) * 64 + lane];
+#pragma unroll
+              for (int t = 0; t < NS; ++t) s[t] = mma<BF16>(kf[t][c][j], b, s[t]);
+            }
+          const float z = s_lse[buf][16 * grp + n];
+          const int see = prefix + s_row[buf][16 * grp + n];  // the last position it sees
+          if (__any(key0 + 16 * NS - 1 > see)) {
+#pragma unroll
+            for (int t = 0; t < NS; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                w[t][i] += key0 + 16 * t + 4 * g + i > see ? 0.0f : exp2_(fmaf(s[t][i], f[t], -z));
+          } else {
+#pragma unroll
+            for (int t = 0; t < NS; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) w[t][i] += exp2_(fmaf(s[t][i], f[t], -z));
+          }
+        }
+      }
+    }
+  }
+  if (!on) return;
+#pragma unroll
+  for (int t = 0; t < NS; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) w[t][i] += __shfl_xor(w[t][i], o);
+      const int pos = key0 + 16 * t + 4 * g + i;
+      if (n == 4 * t % 16 + i && pos < L) weights[(size_t)kv * stride + pos] += w[t][i];
+    }
+}
+
+template <int D, bool BF16>
+hipError_t launch_prefill_t(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q,
+                            int32_t T, int32_t Hq, const int32_t* table, int32_t prefix,
+                            float scale, int n_split, float* ws, void* out, float* lse, int shift,
+                            hipStream_t stream) {
+  const int Hkv = L.num_kv_heads;
+  const int64_t ncols = (int64_t)T * (Hq / Hkv);
+  const int n_rb = (int)((ncols + block_cols<D>() - 1) / block_cols<D>());
+  // a negative scale negates the queries, so that the scores' factors are positive
+  hipLaunchKernelGGL((kv8_prefill_kernel<D, BF16>), dim3((uint32_t)(Hkv * (int64_t)n_rb * n_split)),
+                     dim3(kThreads), 0, stream, static_cast<const uint8_t*>(pool.k_codes),
+                     static_cast<const uint8_t*>(pool.k_meta),
+                     static_cast<const uint8_t*>(pool.v_codes),
+                     static_cast<const uint8_t*>(pool.v_meta), static_cast<const uint16_t*>(q),
+                     table, ws, static_cast<uint16_t*>(out), lse, Hq, Hkv, L.page_size, shift,
+                     L.num_pages, T, prefix, n_rb, n_split, std::fabs(scale) * kLog2e,
+                     scale < 0.0f ? 0x80008000u : 0u);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || n_split == 1) return e;
+  const int64_t threads = ncols * Hkv * (D / 4);
+  hipLaunchKernelGGL((kv8_prefill_combine_kernel<D, BF16>), dim3((uint32_t)((threads + 255) / 256)),
+                     dim3(256), 0, stream, ws, static_cast<uint16_t*>(out), lse, Hq, Hkv, ncols,
+                     n_split);
+  return hipGetLastError();
+}
+
+int shift_of(int block) {
+  int s = 0;
+  while ((1 << s) < block) ++s;
+  return s;
+}
+
+}  // namespace
+
+// Splits of a chunk's tiles: the count with the least estimated time.  A turn
+// of the chip takes the tiles of its longest block and a start and end worth
+// about four; the partials are written and read once, at about 4 TB/s, and
+// joined by a second launch (a tile takes about 1.7 us).
+int kv8_prefill_splits(const jf_kv_layout& L, int32_t T, int32_t Hq, int32_t prefix) {
+  const int cols = L.head_dim == 256 ? block_cols<256>() : L.head_dim == 128 ? block_cols<128>() : block_cols<64>();
+  const int64_t ncols = (int64_t)T * (Hq / L.num_kv_heads);
+  const int64_t blocks = (ncols + cols - 1) / cols * L.num_kv_heads, cus = num_cus();
+  const int64_t tiles = ((int64_t)prefix + T - 1) / kTile + 1;
+  int best = 1;
+  double least = 0.0;
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    const double turns = (double)((blocks * s + cus - 1) / cus);
+    double cost = turns * ((double)((tiles + s - 1) / s) + 4.0);
+    if (s > 1) cost += 2.0 + (double)s * ncols * L.num_kv_heads * (L.head_dim + 4) * 8.0 / 4e12 / 1.7e-6;
+    if (s == 1 || cost < 0.98 * least) least = cost, best = s;
+  }
+  return best;
+}
+
+size_t kv8_prefill_bytes(const jf_kv_layout& L, int32_t T, int32_t Hq, int splits) {
+  return splits <= 1 ? 0 : (size_t)splits * T * Hq * (L.head_dim + 4) * sizeof(float);
+}
+
+hipError_t launch_kv8_prefill(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                              const void* q, int32_t T, int32_t Hq, const int32_t* block_table,
+                              int32_t prefix_len, float softmax_scale, int splits, void* ws,
+                              void* out, float* lse, hipStream_t stream) {
+  auto go = [&](auto fn) {
+    return fn(L, pool, q, T, Hq, block_table, prefix_len, softmax_scale, splits,
+              static_cast<float*>(ws), out, lse, shift_of(L.group_size), stream);
+  };
+  if (L.head_dim == 64) return bf16 ? go(launch_prefill_t<64, true>) : go(launch_prefill_t<64, false>);
+  if (L.head_dim == 128) return bf16 ? go(launch_prefill_t<128, true>) : go(launch_prefill_t<128, false>);
+  return bf16 ? go(launch_prefill_t<256, true>) : go(launch_prefill_t<256, false>);
+}
+
+namespace {
+template <int D, bool BF16, int NS>
+hipError_t launch_weights_t(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q,
+                            const float* lse, int32_t T, int32_t Hq, const int32_t* table,
+                            int32_t prefix, float scale, float* weights, int64_t stride,
+                            hipStream_t stream) {
+  const int64_t keys = (int64_t)prefix + T, per = kWWaves * 16 * NS;
+  hipLaunchKernelGGL((kv8_weights_kernel<D, BF16, NS>),
+                     dim3((uint32_t)((keys + per - 1) / per * L.num_kv_heads)), dim3(kWThreads), 0,
+                     stream, static_cast<const uint8_t*>(pool.k_codes),
+                     static_cast<const uint8_t*>(pool.k_meta), static_cast<const uint16_t*>(q), lse,
+                     table, weights, stride, Hq, L.num_kv_heads, L.page_size,
+                     shift_of(L.group_size), L.num_pages, T, prefix, scale * kLog2e);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_kv8_weights(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                              const void* q, const float* lse, int32_t T, int32_t Hq,
+                              const int32_t* block_table, int32_t prefix_len, float softmax_scale,
+                              float* weights, int64_t stride, hipStream_t stream) {
+  auto go = [&](auto fn) {
+    return fn(L, pool, q, lse, T, Hq, block_table, prefix_len, softmax_scale, weights, stride, stream);
+  };
+  if (L.head_dim == 64) return bf16 ? go(launch_weights_t<64, true, 4>) : go(launch_weights_t<64, false, 4>);
+  if (L.head_dim == 128) return bf16 ? go(launch_weights_t<128, true, 4>) : go(launch_weights_t<128, false, 4>);
+  return bf16 ? go(launch_weights_t<256, true, 4>) : go(launch_weights_t<256, false, 4>);
+}
+
+}  // namespace jfkv

@@ -32,6 +32,9 @@ EXPORTS = [
     "jf_prefill_workspace_bytes", "jf_prefill_attn_q4_ws", "jf_reconstruct_q4", "jf_tq4_pool_bytes", "jf_tq4_encode_append", "jf_tq4_decode_attn",
     "jf_tq4_reconstruct", "jf_kv_page_bytes", "jf_kv_pack_pages", "jf_kv_unpack_pages",
     "jf_snapshot_save", "jf_snapshot_restore", "jf_calib_read_stream",
+    "jf_kv8_pool_bytes", "jf_kv8_append", "jf_kv8_decode_workspace_bytes", "jf_kv8_decode_attn",
+    "jf_kv8_prefill_workspace_bytes", "jf_kv8_prefill_attn", "jf_kv8_attn_weights",
+    "jf_kv8_evict_workspace_bytes", "jf_kv8_evict",
 ]
 
 
@@ -62,7 +65,7 @@ def _load():
         raise ImportError("libjfkv.so is not built (%s); run __graft_entry__.build()" % LIB_PATH)
     L = ctypes.CDLL(LIB_PATH)
     P, i32, u64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_size_t
-    pi32 = ctypes.POINTER(ctypes.c_int32)
+    pi32, i64 = ctypes.POINTER(ctypes.c_int32), ctypes.c_int64
     st = ctypes.c_int
     sig = {
         "jf_last_error": (ctypes.c_char_p, []),
@@ -105,6 +108,18 @@ def _load():
         "jf_tq4_encode_append": (st, [P, P, P, P, P, P, P, P, P, i32, i32, i32, P]),
         "jf_tq4_decode_attn": (st, [P, P, P, P, P, P, P, P, P, i32, i32, P, i32, P,
                                     ctypes.c_float, i32, P, sz, P, P]),
+        "jf_kv8_pool_bytes": (st, [P, ctypes.POINTER(sz), ctypes.POINTER(sz)]),
+        "jf_kv8_append": (st, [P, P, i32, P, P, P, P, P, i32, i32, i32, P]),
+        "jf_kv8_decode_workspace_bytes": (st, [P, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]),
+        "jf_kv8_decode_attn": (st, [P, P, i32, P, i32, i32, i32, P, i32, P, ctypes.c_float, i32, P,
+                                    sz, P, P, i64, P]),
+        "jf_kv8_prefill_workspace_bytes": (st, [P, i32, i32, i32, ctypes.POINTER(sz)]),
+        "jf_kv8_prefill_attn": (st, [P, P, i32, P, i32, i32, P, i32, i32, ctypes.c_float, P, sz, P,
+                                     P, P]),
+        "jf_kv8_attn_weights": (st, [P, P, i32, P, P, i32, i32, P, i32, i32, ctypes.c_float, P, i64,
+                                     P]),
+        "jf_kv8_evict_workspace_bytes": (st, [P, i32, i32, i32, ctypes.POINTER(sz)]),
+        "jf_kv8_evict": (st, [P, P, i32, P, i32, P, P, i64, i32, i32, P, i32, P, sz, P, P, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -826,3 +841,225 @@ def snapshot_restore(path: str, pools, block_table, block_table_host, staging_de
                                    _ptr(staging_dev), _ptr(staging), staging.numel(),
                                    ctypes.byref(n), _stream(stream)))
     return n.value
+
+
+# ---------------------------------------------------------------- 8-bit cache
+JF_F16, JF_BF16 = 0, 1
+
+
+def kv8_pool_bytes(lay: Layout):
+    """(codes, exponents) bytes of one array, the same for K and V; the layout's
+    group_size counts the positions that share an exponent."""
+    cb, eb = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib.jf_kv8_pool_bytes(ctypes.byref(lay), ctypes.byref(cb), ctypes.byref(eb)))
+    return cb.value, eb.value
+
+
+class KV8Pool:
+    """One layer's 8-bit K and V pools in device memory (uint8 e4m3 codes and
+    exponent bytes; see include/jfkv.h).  `tensors`: existing uint8 arrays
+    (k_codes, k_exps, v_codes, v_exps) instead of new ones."""
+
+    def __init__(self, lay: Layout, device="cuda", fill: Optional[int] = None, tensors=None):
+        import torch
+        self.layout = lay
+        sizes = kv8_pool_bytes(lay) * 2
+        if tensors is None:
+            tensors = [torch.empty(n, dtype=torch.uint8, device=device) for n in sizes]
+            if fill is not None:
+                for t in tensors:
+                    t.fill_(fill)
+        for t, n, name in zip(tensors, sizes, ("k_codes", "k_exps", "v_codes", "v_exps")):
+            _dev_check(t, name, torch.uint8)
+            if t.numel() != n:
+                raise ValueError("%s must hold %d bytes, got %d" % (name, n, t.numel()))
+        self.k_codes, self.k_exps, self.v_codes, self.v_exps = tensors
+
+    def ptrs(self) -> PoolPtrs:
+        return PoolPtrs(self.k_codes.data_ptr(), self.k_exps.data_ptr(),
+                        self.v_codes.data_ptr(), self.v_exps.data_ptr())
+
+
+def _kv8_check(pool: KV8Pool, floats=(), ints=(), f32=(), raw=()):
+    """Kind, type and device of a call's tensors, (tensor, name) each; returns
+    the JF_ type of `floats` (fp16 or bf16, all the same)."""
+    import torch
+    dtype = floats[0][0].dtype if floats else torch.float16
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("%s must be float16 or bfloat16, got %s" % (floats[0][1], dtype))
+    here = torch.cuda.current_device() if pool.k_codes.is_cuda else None
+    for group, want in ((floats, dtype), (ints, torch.int32), (f32, torch.float32), (raw, None),
+                        (((pool.k_codes, "pool"),), torch.uint8)):
+        for t, name in group:
+            _dev_check(t, name, want)
+            if t is not None and t.device.index != here:
+                raise ValueError("%s is on %s, the current device is cuda:%s" % (name, t.device, here))
+    return JF_BF16 if dtype == torch.bfloat16 else JF_F16
+
+
+def _kv8_tables(block_tables, B, seq_lens=None):
+    if block_tables.dim() != 2 or block_tables.shape[0] != B:
+        raise ValueError("block_tables must be [B][max_pages]")
+    if seq_lens is not None and tuple(seq_lens.shape) != (B,):
+        raise ValueError("seq_lens must be [B]")
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _size(fn, *args) -> int:
+    n = ctypes.c_size_t()
+    _check(fn(*args, ctypes.byref(n)))
+    return n.value
+
+
+def bind_kv8_append(pool: KV8Pool, k_new, v_new, cu_tok, start_pos, block_tables,
+                    stream=None) -> BoundCall:
+    """jf_kv8_append with its arguments checked and marshalled once."""
+    dt = _kv8_check(pool, ((k_new, "k_new"), (v_new, "v_new")),
+                    ((cu_tok, "cu_tok"), (start_pos, "start_pos"), (block_tables, "block_tables")))
+    lay, ptrs = pool.layout, pool.ptrs()
+    if tuple(k_new.shape[1:]) != (lay.num_kv_heads, lay.head_dim) or v_new.shape != k_new.shape:
+        raise ValueError("k_new/v_new must be [total_tok][Hkv][head_dim]")
+    B = start_pos.shape[0]
+    _kv8_tables(block_tables, B)
+    if tuple(cu_tok.shape) != (B + 1,):
+        raise ValueError("cu_tok must be [B+1]")
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), dt, _ptr(k_new), _ptr(v_new), _ptr(cu_tok),
+            _ptr(start_pos), _ptr(block_tables), B, block_tables.shape[1], k_new.shape[0],
+            _stream(stream))
+    return BoundCall(lib.jf_kv8_append, args,
+                     (lay, ptrs, pool, k_new, v_new, cu_tok, start_pos, block_tables))
+
+
+def jf_kv8_append(pool: KV8Pool, k_new, v_new, cu_tok, start_pos, block_tables, stream=None):
+    """Quantize rows k_new, v_new [total_tok][Hkv][d] (fp16 or bf16) into an 8-bit
+    cache at their logical positions."""
+    bind_kv8_append(pool, k_new, v_new, cu_tok, start_pos, block_tables, stream)()
+
+
+def jf_kv8_decode_workspace_bytes(lay: Layout, B: int, num_queries: int, num_q_heads: int,
+                                  max_splits: int, weight_pages: int = 0) -> int:
+    """weight_pages: pages per request of the tables, for calls that add weights up."""
+    return _size(lib.jf_kv8_decode_workspace_bytes, ctypes.byref(lay), B, num_queries, num_q_heads,
+                 max_splits, weight_pages)
+
+
+def bind_kv8_decode(pool: KV8Pool, q, block_tables, seq_lens, softmax_scale, max_splits, workspace,
+                    out, weights=None, stream=None) -> BoundCall:
+    """jf_kv8_decode_attn with its arguments checked and marshalled once."""
+    dt = _kv8_check(pool, ((q, "q"), (out, "out")),
+                    ((block_tables, "block_tables"), (seq_lens, "seq_lens")),
+                    ((weights, "weights"),), ((workspace, "workspace"),))
+    lay, ptrs = pool.layout, pool.ptrs()
+    if q.dim() != 4 or q.shape[3] != lay.head_dim or out.shape != q.shape:
+        raise ValueError("q/out must be [B][Sq][Hq][head_dim]")
+    B, Sq, Hq, _ = q.shape
+    _kv8_tables(block_tables, B, seq_lens)
+    if weights is not None and (weights.dim() != 3 or tuple(weights.shape[:2]) != (B, lay.num_kv_heads)):
+        raise ValueError("weights must be [B][Hkv][positions]")
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), dt, _ptr(q), B, Sq, Hq, _ptr(block_tables),
+            block_tables.shape[1], _ptr(seq_lens), float(softmax_scale), int(max_splits),
+            _ptr(workspace), _nbytes(workspace), _ptr(out), _ptr(weights),
+            0 if weights is None else weights.shape[2], _stream(stream))
+    return BoundCall(lib.jf_kv8_decode_attn, args,
+                     (lay, ptrs, pool, q, block_tables, seq_lens, workspace, out, weights))
+
+
+def jf_kv8_decode_attn(pool: KV8Pool, q, block_tables, seq_lens, softmax_scale: float,
+                       max_splits: int, workspace, out, weights=None, stream=None):
+    """Decode over the 8-bit cache: q, out [B][Sq][Hq][d] (Sq = 1..4 causal tokens
+    at the end of each request); weights fp32 [B][Hkv][positions] grow by the
+    call's attention weights."""
+    bind_kv8_decode(pool, q, block_tables, seq_lens, softmax_scale, max_splits, workspace, out,
+                    weights, stream)()
+
+
+def jf_kv8_prefill_workspace_bytes(lay: Layout, T: int, num_q_heads: int, prefix_len: int) -> int:
+    return _size(lib.jf_kv8_prefill_workspace_bytes, ctypes.byref(lay), T, num_q_heads, prefix_len)
+
+
+def bind_kv8_prefill(pool: KV8Pool, q, block_table, prefix_len: int, softmax_scale, out, lse=None,
+                     workspace=None, stream=None) -> BoundCall:
+    """jf_kv8_prefill_attn with its arguments checked and marshalled once."""
+    dt = _kv8_check(pool, ((q, "q"), (out, "out")), ((block_table, "block_table"),),
+                    ((lse, "lse"),), ((workspace, "workspace"),))
+    lay, ptrs = pool.layout, pool.ptrs()
+    if q.dim() != 3 or q.shape[2] != lay.head_dim or out.shape != q.shape:
+        raise ValueError("q/out must be [T][Hq][head_dim]")
+    if block_table.dim() != 1 or (lse is not None and lse.shape != q.shape[:2]):
+        raise ValueError("block_table must be [max_pages], lse [T][Hq]")
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), dt, _ptr(q), q.shape[0], q.shape[1],
+            _ptr(block_table), block_table.shape[0], int(prefix_len), float(softmax_scale),
+            _ptr(workspace) or None, _nbytes(workspace), _ptr(out), _ptr(lse), _stream(stream))
+    return BoundCall(lib.jf_kv8_prefill_attn, args,
+                     (lay, ptrs, pool, q, block_table, out, lse, workspace))
+
+
+def jf_kv8_prefill_attn(pool: KV8Pool, q, block_table, prefix_len: int, softmax_scale: float, out,
+                        lse=None, workspace=None, stream=None):
+    """Rows q, out [T][Hq][d] at positions prefix_len .. prefix_len + T - 1, which
+    are in the cache already, attend causally to it; lse fp32 [T][Hq].  workspace:
+    jf_kv8_prefill_workspace_bytes() bytes; without it the keys of a chunk of few
+    rows are not shared among more blocks."""
+    bind_kv8_prefill(pool, q, block_table, prefix_len, softmax_scale, out, lse, workspace, stream)()
+
+
+def bind_kv8_attn_weights(pool: KV8Pool, q, lse, block_table, prefix_len: int, softmax_scale,
+                          weights, stream=None) -> BoundCall:
+    """jf_kv8_attn_weights with its arguments checked and marshalled once."""
+    dt = _kv8_check(pool, ((q, "q"),), ((block_table, "block_table"),),
+                    ((lse, "lse"), (weights, "weights")))
+    lay, ptrs = pool.layout, pool.ptrs()
+    if q.dim() != 3 or q.shape[2] != lay.head_dim or lse.shape != q.shape[:2]:
+        raise ValueError("q must be [T][Hq][head_dim], lse [T][Hq]")
+    if block_table.dim() != 1 or weights.dim() != 2 or weights.shape[0] != lay.num_kv_heads:
+        raise ValueError("block_table must be [max_pages], weights [Hkv][positions]")
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), dt, _ptr(q), _ptr(lse), q.shape[0], q.shape[1],
+            _ptr(block_table), block_table.shape[0], int(prefix_len), float(softmax_scale),
+            _ptr(weights), weights.shape[1], _stream(stream))
+    return BoundCall(lib.jf_kv8_attn_weights, args, (lay, ptrs, pool, q, lse, block_table, weights))
+
+
+def jf_kv8_attn_weights(pool: KV8Pool, q, lse, block_table, prefix_len: int, softmax_scale: float,
+                        weights, stream=None):
+    """Adds the attention weights of rows q [T][Hq][d], with the lse [T][Hq] that
+    jf_kv8_prefill_attn left for them, to weights fp32 [Hkv][positions]."""
+    bind_kv8_attn_weights(pool, q, lse, block_table, prefix_len, softmax_scale, weights, stream)()
+
+
+def jf_kv8_evict_workspace_bytes(lay: Layout, B: int, max_pages: int, keep: int) -> int:
+    return _size(lib.jf_kv8_evict_workspace_bytes, ctypes.byref(lay), B, max_pages, keep)
+
+
+def bind_kv8_evict(pool: KV8Pool, block_tables, seq_lens, weights, keep: int, recent: int,
+                   dst_tables, workspace, kept, kept_weights, stream=None) -> BoundCall:
+    """jf_kv8_evict with its arguments checked and marshalled once."""
+    _kv8_check(pool, (), ((block_tables, "block_tables"), (seq_lens, "seq_lens"),
+                          (dst_tables, "dst_tables"), (kept, "kept")),
+               ((weights, "weights"), (kept_weights, "kept_weights")), ((workspace, "workspace"),))
+    lay, ptrs = pool.layout, pool.ptrs()
+    B = seq_lens.shape[0]
+    _kv8_tables(block_tables, B, seq_lens)
+    if dst_tables.dim() != 2 or dst_tables.shape[0] != B:
+        raise ValueError("dst_tables must be [B][dst_max_pages]")
+    if weights.dim() != 3 or tuple(weights.shape[:2]) != (B, lay.num_kv_heads):
+        raise ValueError("weights must be [B][Hkv][positions]")
+    if tuple(kept.shape) != (B, lay.num_kv_heads, keep) or kept_weights.shape != kept.shape:
+        raise ValueError("kept and kept_weights must be [B][Hkv][keep]")
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), B, _ptr(block_tables), block_tables.shape[1],
+            _ptr(seq_lens), _ptr(weights), weights.shape[2], int(keep), int(recent),
+            _ptr(dst_tables), dst_tables.shape[1], _ptr(workspace) or None, _nbytes(workspace),
+            _ptr(kept), _ptr(kept_weights), _stream(stream))
+    return BoundCall(lib.jf_kv8_evict, args, (lay, ptrs, pool, block_tables, seq_lens, weights,
+                                              dst_tables, workspace, kept, kept_weights))
+
+
+def jf_kv8_evict(pool: KV8Pool, block_tables, seq_lens, weights, keep: int, recent: int, dst_tables,
+                 workspace, kept, kept_weights, stream=None):
+    """Moves, for each request and KV head, the last `recent` positions and those
+    of the largest weights, min(length, keep) in all, in order into the pages of
+    dst_tables; kept int32 and kept_weights fp32 [B][Hkv][keep] say which."""
+    bind_kv8_evict(pool, block_tables, seq_lens, weights, keep, recent, dst_tables, workspace, kept,
+                   kept_weights, stream)()
