@@ -161,12 +161,15 @@ hipError_t launch_kv8_weights(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool
                               const int32_t* block_table, int32_t prefix_len, float softmax_scale,
                               float* weights, int64_t stride, hipStream_t stream);
 
-// Eviction into the pages of dst_tables; kept, kept_w [B][Hkv][keep].
+// Eviction into the pages of dst_tables; kept, kept_w [B][Hkv][keep]; ws of
+// kv8_evict_bytes() bytes.
+size_t kv8_evict_bytes(const jf_kv_layout& L, int32_t B, int32_t max_pages);
 hipError_t launch_kv8_evict(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, int32_t B,
                             const int32_t* block_tables, int32_t max_pages,
                             const int32_t* seq_lens, const float* weights, int64_t stride,
                             int32_t keep, int32_t recent, const int32_t* dst_tables,
-                            int32_t dst_pages, int32_t* kept, float* kept_w, hipStream_t stream);
+                            int32_t dst_pages, void* ws, int32_t* kept, float* kept_w,
+                            hipStream_t stream);
 
 // Read-rate calibration: one pass over bytes (a multiple of 16) of buf.
 hipError_t launch_read_stream(const void* buf, size_t bytes, int32_t blocks, uint32_t* sink,

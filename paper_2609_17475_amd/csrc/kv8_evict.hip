@@ -18,8 +18,13 @@ namespace {
 
 using namespace kv8;
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelWaves = kSelThreads / 64;
+constexpr int kBins = 2048;      // 11 bits of rank at a time
+constexpr int kPerLane = 16;     // positions per lane; a wave holds 1,024 in a row
+constexpr int kWavePos = 64 * kPerLane;
+constexpr int kOneThreads = 1024;                           // rows of one workgroup
+constexpr int kOnePos = kOneThreads * kPerLane;             // at most 16,384 positions
+constexpr int kPartThreads = 512;                           // longer rows: parts of
+constexpr int kPartPos = kPartThreads * kPerLane;           // 8,192 positions
 
 // Weights in an order of unsigned integers: -inf lowest, then by value (-0 as
 // +0), every NaN highest.
@@ -30,81 +35,248 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// One workgroup per (request, KV head): radix selection of the threshold among
-// the positions before the recent ones (four passes of eight bits over their
-// ranks), then one pass that writes the kept positions in order.
-__global__ __launch_bounds__(kSelThreads) void kv8_select_kernel(
+// What one (request, KV head) keeps: m of n positions, the last n - cand for sure
+// and `need` of the cand before them.
+struct Quota {
+  int n, m, cand;
+  uint32_t need;
+};
+__device__ __forceinline__ Quota quota_of(int len, int cap, int keep, int recent) {
+  const int n = min(max(len, 0), cap), m = min(n, keep), r = min(recent, n);
+  return {n, m, n - r, (uint32_t)(m - r)};
+}
+
+// The ranks of the wave's positions first + 64 k + lane (0 from n on).
+__device__ __forceinline__ void load_ranks(uint32_t (&rank)[kPerLane], float (&w)[kPerLane],
+                                           const float* row, int first, int lane, int n) {
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) {
+    const int i = first + 64 * k + lane;
+    w[k] = i < n ? row[i] : 0.0f;
+  }
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) rank[k] = rank_of(w[k]);
+}
+
+// Counts the digits (bits shift ..) of the candidates whose higher bits are
+// those of limit.  Lanes that share the first such lane's digit are counted in
+// one addition (equal weights would serialize the atomics).
+__device__ __forceinline__ void count_digits(uint32_t* hist, const uint32_t (&rank)[kPerLane],
+                                             int first, int lane, int cand, uint32_t known,
+                                             uint32_t limit, int shift) {
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) {
+    bool on = first + 64 * k + lane < cand && (rank[k] & known) == limit;
+    const uint32_t d = (rank[k] >> shift) & (kBins - 1);
+    const uint64_t any = __ballot(on);
+    if (!any) continue;
+    const int lead = __builtin_ctzll(any);
+    const uint64_t same = __ballot(on && d == (uint32_t)__builtin_amdgcn_readlane((int)d, lead));
+    if (lane == lead)
+      atomicAdd(&hist[d], (uint32_t)__popcll(same));
+    else if (on && !(same >> lane & 1))
+      atomicAdd(&hist[d], 1u);
+  }
+}
+
+// The largest digit d with need <= counts of digits >= d, and what need leaves
+// for d itself.  One workgroup of NT threads; scratch: NT / 64 + 2 words of LDS.
+template <int NT>
+__device__ __forceinline__ void find_digit(const uint32_t* hist, uint32_t need, uint32_t* scratch,
+                                           uint32_t& digit, uint32_t& left) {
+  constexpr int kPer = kBins / NT, kW = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t c[kPer], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) sum += c[j] = hist[kBins - 1 - (tid * kPer + j)];
+  uint32_t upto = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t up = __shfl_up(upto, o);
+    if (lane >= o) upto += up;
+  }
+  if (lane == 63) scratch[wave] = upto;
+  __syncthreads();
+  for (int v = 0; v < wave; ++v) upto += scratch[v];
+  uint32_t before = upto - sum;
+  if (before < need && need <= upto) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (before < need && need <= before + c[j]) {
+        scratch[kW] = kBins - 1 - (tid * kPer + j);
+        scratch[kW + 1] = need - before;
+      }
+      before += c[j];
+    }
+  }
+  __syncthreads();
+  digit = scratch[kW], left = scratch[kW + 1];
+  __syncthreads();
+}
+
+constexpr int kShifts[3] = {21, 10, 0};
+__device__ __forceinline__ uint32_t known_bits(int level) {  // before this level
+  return level == 0 ? 0u : level == 1 ? 0xffe00000u : 0xfffffc00u;
+}
+
+// Which positions of the wave stay, written in order.  sure0, equal0: positions
+// above and at the limit before the wave's (the recent ones count as above).
+__device__ __forceinline__ void count_kept(const uint32_t (&rank)[kPerLane], int first, int lane,
+                                           const Quota& t, uint32_t limit, uint32_t& sure,
+                                           uint32_t& equal) {
+  sure = equal = 0;
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) {
+    const int i = first + 64 * k + lane;
+    sure += __popcll(__ballot(i < t.n && (i >= t.cand || (t.need && rank[k] > limit))));
+    equal += __popcll(__ballot(t.need && i < t.cand && rank[k] == limit));
+  }
+}
+__device__ __forceinline__ void write_kept(const uint32_t (&rank)[kPerLane],
+                                           const float (&w)[kPerLane], int first, int lane,
+                                           const Quota& t, uint32_t limit, uint32_t stay,
+                                           uint32_t sure0, uint32_t equal0, int32_t* out,
+                                           float* out_w) {
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int k = 0; k < kPerLane; ++k) {
+    const int i = first + 64 * k + lane;
+    const bool sure = i < t.n && (i >= t.cand || (t.need && rank[k] > limit));
+    const bool same = t.need && i < t.cand && rank[k] == limit;
+    const uint64_t bs = __ballot(sure), be = __ballot(same);
+    const uint32_t eq = equal0 + __popcll(be & below);
+    if (sure || (same && eq < stay)) {
+      const uint32_t to = sure0 + __popcll(bs & below) + min(eq, stay);
+      out[to] = i, out_w[to] = w[k];
+    }
+    sure0 += __popcll(bs), equal0 += __popcll(be);
+  }
+}
+
+// Rows of at most 16,384 positions: one workgroup each, the ranks in registers
+// from the first histogram to the output.
+__global__ __launch_bounds__(kOneThreads) void kv8_select_kernel(
     const int32_t* __restrict__ seq_lens, const float* __restrict__ weights, int64_t stride, int cap,
     int keep, int recent, int32_t* __restrict__ kept, float* __restrict__ kept_w) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t s_digit, s_need;
-  __shared__ uint32_t s_gt[kSelWaves], s_eq[kSelWaves];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int kv = blockIdx.x, b = blockIdx.y, Hkv = gridDim.x;
-  const size_t row = (size_t)b * Hkv + kv;
-  const float* w = weights + row * stride;
+  constexpr int kW = kOneThreads / 64;
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t scratch[kW + 2];
+  __shared__ uint32_t s_sure[kW], s_equal[kW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = wave * kWavePos;
+  const size_t row = (size_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const Quota t = quota_of(seq_lens[blockIdx.y], cap, keep, recent);
+  uint32_t rank[kPerLane];
+  float w[kPerLane];
+  load_ranks(rank, w, weights + row * stride, first, lane, t.n);
+  uint32_t limit = 0, stay = t.need;
+  if (t.need)
+    for (int level = 0; level < 3; ++level) {
+      for (int i = tid; i < kBins; i += kOneThreads) hist[i] = 0;
+      __syncthreads();
+      count_digits(hist, rank, first, lane, t.cand, known_bits(level), limit, kShifts[level]);
+      __syncthreads();
+      uint32_t d;
+      find_digit<kOneThreads>(hist, stay, scratch, d, stay);
+      limit |= d << kShifts[level];
+    }
+  uint32_t sure, equal, sure0 = 0, equal0 = 0;
+  count_kept(rank, first, lane, t, limit, sure, equal);
+  if (lane == 0) s_sure[wave] = sure, s_equal[wave] = equal;
+  __syncthreads();
+  for (int v = 0; v < wave; ++v) sure0 += s_sure[v], equal0 += s_equal[v];
   int32_t* out = kept + row * keep;
   float* out_w = kept_w + row * keep;
+  write_kept(rank, w, first, lane, t, limit, stay, sure0, equal0, out, out_w);
+  for (int j = t.m + tid; j < keep; j += kOneThreads) out[j] = -1, out_w[j] = 0.0f;
+}
 
-  const int n = min(max(seq_lens[b], 0), cap);
-  const int m = min(n, keep), r = min(recent, n);
-  const int cand = n - r;       // positions that compete
-  uint32_t need = m - r;        // how many of them stay
+// Longer rows: parts of 8,192 positions, one launch per step.  Workspace of a
+// row: three histograms, the (limit, stay) after each, and every part's counts.
+struct RowState {
+  uint32_t hist[3][kBins];
+  uint32_t limit[3], stay[3];
+};
+__device__ __forceinline__ RowState* state_of(void* ws, size_t row, int parts) {
+  return reinterpret_cast<RowState*>(static_cast<uint8_t*>(ws) +
+                                     row * (sizeof(RowState) + sizeof(uint2) * parts));
+}
 
-  // threshold: the need-th largest rank; `need` becomes how many of its equals stay
-  uint32_t limit = 0, known = 0;
-  if (need > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < cand; i += kSelThreads) {
-        const uint32_t k = rank_of(w[i]);
-        if ((k & known) == limit) atomicAdd(&hist[(k >> shift) & 255], 1u);
+__global__ void kv8_select_clear_kernel(void* ws, int parts) {
+  uint32_t* h = &state_of(ws, blockIdx.x, parts)->hist[0][0];
+  for (int i = threadIdx.x; i < 3 * kBins; i += blockDim.x) h[i] = 0;
+}
+
+// Level 0..2: the part's digits into the row's histogram of that level (after
+// the previous level's digit was found, by every part alike).  Level 3: the
+// part's counts.  Level 4: its kept positions.
+template <int LEVEL>
+__global__ __launch_bounds__(kPartThreads) void kv8_select_part_kernel(
+    const int32_t* __restrict__ seq_lens, const float* __restrict__ weights, int64_t stride, int cap,
+    int keep, int recent, int32_t* __restrict__ kept, float* __restrict__ kept_w, void* ws) {
+  constexpr int kW = kPartThreads / 64;
+  __shared__ uint32_t hist[LEVEL < 3 ? kBins : 1];
+  __shared__ uint32_t scratch[kW + 2];
+  __shared__ uint32_t s_sure[kW], s_equal[kW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int part = blockIdx.x, parts = gridDim.x;
+  const size_t row = (size_t)blockIdx.z * gridDim.y + blockIdx.y;
+  const Quota t = quota_of(seq_lens[blockIdx.z], cap, keep, recent);
+  RowState* st = state_of(ws, row, parts);
+  uint2* counts = reinterpret_cast<uint2*>(st + 1);
+  if constexpr (LEVEL == 4) {  // (this also where the row has no such part)
+    for (int j = t.m + part * kPartThreads + tid; j < keep; j += parts * kPartThreads)
+      kept[row * keep + j] = -1, kept_w[row * keep + j] = 0.0f;
+  }
+  const int base = part * kPartPos;
+  if (base >= t.n) return;
+  const int first = base + wave * kWavePos;
+  uint32_t rank[kPerLane];
+  float w[kPerLane];
+  load_ranks(rank, w, weights + row * stride, first, lane, t.n);
+
+  uint32_t limit = 0, stay = t.need;
+  if constexpr (LEVEL > 0) {
+    if (t.need) {
+      if constexpr (LEVEL > 1 && LEVEL < 4) limit = st->limit[LEVEL - 2], stay = st->stay[LEVEL - 2];
+      if constexpr (LEVEL < 4) {
+        uint32_t d;
+        find_digit<kPartThreads>(st->hist[LEVEL - 1], stay, scratch, d, stay);
+        limit |= d << kShifts[LEVEL - 1];
+        if (part == 0 && tid == 0) st->limit[LEVEL - 1] = limit, st->stay[LEVEL - 1] = stay;
+      } else {
+        limit = st->limit[2], stay = st->stay[2];
       }
-      __syncthreads();
-      if (tid == 0) {
-        uint32_t left = need, d = 255;
-        while (hist[d] < left) left -= hist[d--];
-        s_digit = d, s_need = left;
-      }
-      __syncthreads();
-      limit |= s_digit << shift;
-      known |= 255u << shift;
-      need = s_need;
-      __syncthreads();
     }
+  }
+  if constexpr (LEVEL < 3) {
+    if (!t.need || base >= t.cand) return;
+    for (int i = tid; i < kBins; i += kPartThreads) hist[i] = 0;
+    __syncthreads();
+    count_digits(hist, rank, first, lane, t.cand, known_bits(LEVEL), limit, kShifts[LEVEL]);
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kPartThreads)
+      if (hist[i]) atomicAdd(&st->hist[LEVEL][i], hist[i]);
   } else {
-    limit = 0xffffffffu;  // (and no equal stays)
-  }
-
-  uint32_t at = 0, eq_at = 0;  // kept and equal positions so far
-  for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    const float wi = i < n ? w[i] : 0.0f;
-    const uint32_t k = rank_of(wi);
-    const bool sure = i < n && (i >= cand || (m > r && k > limit));
-    const bool equal = i < cand && m > r && k == limit;
-    const uint64_t eq = __ballot(equal);
-    if (lane == 0) s_eq[wave] = __popcll(eq);
+    uint32_t sure, equal;
+    count_kept(rank, first, lane, t, limit, sure, equal);
+    if (lane == 0) s_sure[wave] = sure, s_equal[wave] = equal;
     __syncthreads();
-    uint32_t before = eq_at;
-    for (int v = 0; v < wave; ++v) before += s_eq[v];
-    const uint32_t rank = before + __popcll(eq & ((1ull << lane) - 1));
-    const bool stay = sure || (equal && rank < need);
-    const uint64_t gt = __ballot(stay);
-    if (lane == 0) s_gt[wave] = __popcll(gt);
-    __syncthreads();
-    uint32_t to = at;
-    for (int v = 0; v < kSelWaves; ++v) {
-      if (v < wave) to += s_gt[v];
-      at += s_gt[v];
-      eq_at += s_eq[v];
+    if constexpr (LEVEL == 3) {
+      if (tid == 0) {
+        uint2 c = make_uint2(0u, 0u);
+        for (int v = 0; v < kW; ++v) c.x += s_sure[v], c.y += s_equal[v];
+        counts[part] = c;
+      }
+    } else {
+      uint32_t sure0 = 0, equal0 = 0;
+      for (int j = lane; j < part; j += 64) sure0 += counts[j].x, equal0 += counts[j].y;
+#pragma unroll
+      for (int o = 32; o; o >>= 1) sure0 += __shfl_xor(sure0, o), equal0 += __shfl_xor(equal0, o);
+      for (int v = 0; v < wave; ++v) sure0 += s_sure[v], equal0 += s_equal[v];
+      write_kept(rank, w, first, lane, t, limit, stay, sure0, equal0, kept + row * keep,
+                 kept_w + row * keep);
     }
-    to += __popcll(gt & ((1ull << lane) - 1));
-    if (stay) out[to] = i, out_w[to] = wi;
-    __syncthreads();
   }
-  for (int j = m + tid; j < keep; j += kSelThreads) out[j] = -1, out_w[j] = 0.0f;
 }
 
 // One workgroup per block of destination tokens, KV head and request, for K or
@@ -223,18 +395,43 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
   if (tid == 0) exps[run * (P / block) + j0 % P / block] = (uint8_t)(top + 127);
 }
 
+// Parts of a row of up to cap positions, 0: one workgroup takes it whole.
+int select_parts(int64_t cap) {
+  return cap <= kOnePos ? 0 : (int)((cap + kPartPos - 1) / kPartPos);
+}
+
 }  // namespace
+
+size_t kv8_evict_bytes(const jf_kv_layout& L, int32_t B, int32_t max_pages) {
+  const int parts = select_parts((int64_t)max_pages * L.page_size);
+  return parts ? (size_t)B * L.num_kv_heads * (sizeof(RowState) + sizeof(uint2) * parts) : 0;
+}
 
 hipError_t launch_kv8_evict(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, int32_t B,
                             const int32_t* block_tables, int32_t max_pages,
                             const int32_t* seq_lens, const float* weights, int64_t stride,
                             int32_t keep, int32_t recent, const int32_t* dst_tables,
-                            int32_t dst_pages, int32_t* kept, float* kept_w, hipStream_t stream) {
+                            int32_t dst_pages, void* ws, int32_t* kept, float* kept_w,
+                            hipStream_t stream) {
   const int block = L.group_size, items = block * L.head_dim / 16;
   const int threads = std::min(items, 256);
-  hipLaunchKernelGGL(kv8_select_kernel, dim3(L.num_kv_heads, B), dim3(kSelThreads), 0, stream,
-                     seq_lens, weights, stride, max_pages * L.page_size, keep, recent, kept, kept_w);
-  hipError_t e = hipGetLastError();
+  const int cap = max_pages * L.page_size, Hkv = L.num_kv_heads, parts = select_parts(cap);
+  if (!parts) {
+    hipLaunchKernelGGL(kv8_select_kernel, dim3(Hkv, B), dim3(kOneThreads), 0, stream, seq_lens,
+                       weights, stride, cap, keep, recent, kept, kept_w);
+  } else {
+    hipLaunchKernelGGL(kv8_select_clear_kernel, dim3(Hkv * B), dim3(256), 0, stream, ws, parts);
+    auto step = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3(parts, Hkv, B), dim3(kPartThreads), 0, stream, seq_lens,
+                         weights, stride, cap, keep, recent, kept, kept_w, ws);
+    };
+    step(kv8_select_part_kernel<0>);
+    step(kv8_select_part_kernel<1>);
+    step(kv8_select_part_kernel<2>);
+    step(kv8_select_part_kernel<3>);
+    step(kv8_select_part_kernel<4>);
+  }
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid(2u * (uint32_t)((keep + block - 1) / block), L.num_kv_heads, B);
   auto go = [&](auto kernel) {

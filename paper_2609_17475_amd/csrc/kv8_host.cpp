@@ -68,7 +68,7 @@ jf_status check_heads(const jf_kv_layout* L, int32_t num_q_heads) {
 // the last tile).
 jf_status check_tables(const jf_kv_layout* L, int32_t B, int32_t max_pages) {
   if (B <= 0 || max_pages <= 0) return fail(JF_ERR_INVALID, "B and max_pages must be positive");
-  if ((int64_t)max_pages * L->page_size > INT32_MAX - 4096)
+  if ((int64_t)max_pages * L->page_size > INT32_MAX - 16384)
     return fail(JF_ERR_INVALID, "max_pages * page_size overflows int32");
   return JF_OK;
 }
@@ -78,7 +78,7 @@ jf_status check_chunk(const jf_kv_layout* L, int32_t T, int32_t num_q_heads, int
   if (T < 0 || prefix_len < 0) return fail(JF_ERR_INVALID, "negative size");
   jf_status st = check_heads(L, num_q_heads);
   if (st) return st;
-  if ((int64_t)prefix_len + T > INT32_MAX - 4096)
+  if ((int64_t)prefix_len + T > INT32_MAX - 16384)
     return fail(JF_ERR_INVALID, "prefix_len + T overflows int32");
   if ((int64_t)T * num_q_heads > INT32_MAX || (int64_t)T * num_q_heads * (L->head_dim / 4) > kMaxThreads ||
       ((int64_t)prefix_len + T + 255) * L->num_kv_heads > kMaxThreads)
@@ -133,7 +133,7 @@ jf_status jf_kv8_decode_workspace_bytes(const jf_kv_layout* layout, int32_t B, i
   if (st) return st;
   if (!bytes) return fail(JF_ERR_INVALID, "NULL output pointer");
   if (B <= 0 || weight_pages < 0) return fail(JF_ERR_INVALID, "B must be positive, weight_pages >= 0");
-  if ((int64_t)weight_pages * layout->page_size > INT32_MAX - 4096)
+  if ((int64_t)weight_pages * layout->page_size > INT32_MAX - 16384)
     return fail(JF_ERR_INVALID, "weight_pages * page_size overflows int32");
   if ((st = check_heads(layout, num_q_heads))) return st;
   if (num_queries < 1 || num_queries > 4)
@@ -252,7 +252,8 @@ jf_status jf_kv8_evict_workspace_bytes(const jf_kv_layout* layout, int32_t B, in
   if ((st = check_tables(layout, B, max_pages))) return st;
   if (keep <= 0) return fail(JF_ERR_INVALID, "keep must be positive");
   if (!bytes) return fail(JF_ERR_INVALID, "NULL output pointer");
-  *bytes = 0;
+  if (B > kMaxGridYZ) return fail(JF_ERR_UNSUPPORTED, "B above %d", kMaxGridYZ);
+  *bytes = jfkv::kv8_evict_bytes(*layout, B, max_pages);
   return ok();
 }
 
@@ -272,7 +273,8 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool, 
   if (dst_max_pages <= 0 || (int64_t)dst_max_pages * layout->page_size < keep)
     return fail(JF_ERR_INVALID, "keep %d exceeds dst_max_pages %d * page_size %d", keep, dst_max_pages,
                 layout->page_size);
-  if (B > kMaxGridYZ) return fail(JF_ERR_UNSUPPORTED, "B above %d", kMaxGridYZ);
+  if ((int64_t)B * layout->num_kv_heads * 256 > kMaxThreads)
+    return fail(JF_ERR_UNSUPPORTED, "B * num_kv_heads too large for one launch");
   if (!block_tables || !seq_lens || !weights || !dst_tables || !kept || !kept_weights ||
       (need && !workspace))
     return fail(JF_ERR_INVALID, "NULL device pointer");
@@ -284,6 +286,7 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool, 
     return fail(JF_ERR_INVALID, "weights_stride below max_pages * page_size");
   return device_status(jfkv::launch_kv8_evict(*layout, *pool, B, block_tables, max_pages, seq_lens,
                                               weights, weights_stride, keep, recent, dst_tables,
-                                              dst_max_pages, kept, kept_weights, stream),
+                                              dst_max_pages, workspace, kept, kept_weights,
+                                              stream),
                        "kv8 evict launch");
 }

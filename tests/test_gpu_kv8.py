@@ -377,6 +377,8 @@ def evict(p, tables, lens, w, keep, recent, dst):
     (256, 2, 128, 64, [3000, 2999], 600, 33),
     (64, 1, 64, 16, [90], 200, 40),
     (64, 2, 128, 16, [5000], 17, 1),
+    (256, 2, 64, 128, [20000, 300, 16385], 5000, 100),
+    (256, 1, 64, 64, [33000], 17, 0),
 ])
 @pytest.mark.parametrize("kind", ["spread", "equal", "odd"])
 def test_evict(P, hkv, d, block, lens, keep, recent, kind):
