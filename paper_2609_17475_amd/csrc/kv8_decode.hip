@@ -34,11 +34,12 @@ namespace {
 
 using namespace kv8;
 
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRow = 32;       // positions a wave takes at a time (in one page)
 constexpr int kCols = 16;      // (token, head) pairs of a block
 constexpr int kXcds = 8;
+constexpr int kGroups = 16;    // groups of splits that are joined first, at most
 constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
 constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
 constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
@@ -64,15 +65,15 @@ __device__ __forceinline__ float col_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-template <int D, bool BF16, bool SUMS>
-__global__ __launch_bounds__(kThreads) void kv8_decode_kernel(
+template <int D, bool BF16, bool SUMS, int CS>
+__global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 1 : 3) void kv8_decode_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
     const uint16_t* __restrict__ q, const int32_t* __restrict__ block_tables,
     const int32_t* __restrict__ seq_lens, uint32_t* __restrict__ tickets, float* __restrict__ recs,
     float* __restrict__ lse, float* __restrict__ logits, uint16_t* __restrict__ out, int Hq, int sq,
     int Hkv, int P, int block_shift, int num_pages, int max_pages, int max_splits, int split_cap,
-    int n_hchunks, float scale_log2) {
+    int n_hchunks, int group_splits, float scale_log2) {
   constexpr int C = D / 64;
   constexpr int kPart = D + 4;  // floats of a partial: o, m, l (16-byte rows)
   extern __shared__ __align__(16) float smem[];
@@ -87,37 +88,46 @@ __global__ __launch_bounds__(kThreads) void kv8_decode_kernel(
   if (slot_id >= slots) return;
   const int kv = slot_id % Hkv, split = slot_id / Hkv, b = blockIdx.y;
   const int gq = Hq / Hkv, pairs = gq * sq;
-  const int c0 = hc * kCols, ncols = min(kCols, pairs - c0);
+  const int c0 = hc * kCols * CS, ncols = min(kCols * CS, pairs - c0);
 
   const int L = min(max(seq_lens[b], 0), max_pages * P);
   const int rows = (L + kRow - 1) / kRow;
-  const int S = max(1, min(split_cap, (rows + kWaves - 1) / kWaves));
+  // Rows per wave below which a request is not cut further: every split costs a
+  // start, a merge and a record.  24/4 heads, d = 256, 2 / 3 / 4 rows: 4 x 20,000
+  // positions 48 / 46 / 43 us (3 query tokens 76 / 67 / 61), 4,097 13.6 / 15.2 /
+  // 16.5; 32/8 heads, d = 128: 8 x 9,000 41 / 38 / 39, 4,097 9.6 / 9.4 / 10.0.
+  constexpr int kMinRows = D > 128 && CS > 1 ? 4 : 3;
+  const int S = max(1, min(split_cap, (rows + kWaves * kMinRows - 1) / (kWaves * kMinRows)));
   if (split >= S) return;
   const int base = rows / S, rem = rows % S;
   const int r0 = split * base + min(split, rem), r1 = r0 + base + (split < rem ? 1 : 0);
 
-  // ---- the block's queries as B operands: column n, dims 64 c + 16 g + 8 j ..
-  const int pair = c0 + min(n, ncols - 1);  // (columns without a pair repeat the last one)
-  const int tok = pair / gq, head = kv * gq + pair % gq;
-  const int see = L - sq + 1 + tok;  // positions the column's query sees
-  u32x4 qf[C][2];
-  {
+  // ---- the block's queries as B operands: column n of each set, dims 64 c +
+  // 16 g + 8 j ..
+  int see[CS];  // positions the columns' queries see
+  u32x4 qf[CS][C][2];
+#pragma unroll
+  for (int cs = 0; cs < CS; ++cs) {
+    const int pair = c0 + min(kCols * cs + n, ncols - 1);  // (columns without a pair repeat the last one)
+    const int tok = pair / gq, head = kv * gq + pair % gq;
+    see[cs] = L - sq + 1 + tok;
     const uint16_t* qp = q + (((size_t)b * sq + tok) * Hq + head) * D;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        qf[c][j] = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j);
+        qf[cs][c][j] = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j);
   }
 
-  f32x4 acc[C][4] = {};
-  float m = -INFINITY, l = 0.0f;
+  f32x4 acc[CS][C][4] = {};
+  float m[CS], l[CS];
+#pragma unroll
+  for (int cs = 0; cs < CS; ++cs) m[cs] = -INFINITY, l[cs] = 0.0f;
   int e_ref = 0, e_top = -1000;
 
-  // ---- page walk: the wave takes rows r0 + wave, + kWaves, ...  NB rows are in
-  // flight: a row's registers are refilled with the row NB turns ahead, K's as
-  // soon as the scores are formed and V's after the value products.  Page IDs
-  // are read one turn before the loads that need them.
+  // ---- page walk: the wave takes rows r0 + wave, + kWaves, ...  A row's registers
+  // are refilled with the next row, K's as soon as the scores are formed and V's
+  // after the value products.  Page IDs are read one turn before the loads.
   const int32_t* const table = block_tables + (size_t)b * max_pages;
   const uint32_t koff = n * D + 16 * g, voff = lane * 16;
   const int last = max(r1, 1) - 1;  // (rows past the end read the last one again)
@@ -149,112 +159,148 @@ __global__ __launch_bounds__(kThreads) void kv8_decode_kernel(
             reinterpret_cast<const u32x4*>(vp + voff + t * 16 * D + c * 1024));
   };
 
+  // a row's scores to the workspace, for the sums of the weights
+  auto keep_scores = [&](int r, const float (&s)[CS][2][4]) {
+#pragma unroll
+    for (int cs = 0; cs < CS; ++cs)
+      if (kCols * cs + n < ncols) {
+        float* const lg = logits + (((size_t)b * Hkv + kv) * pairs + c0 + kCols * cs + n) *
+                                       ((size_t)max_pages * P) + r * kRow + 4 * g;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          *reinterpret_cast<f32x4*>(lg + 16 * t) =
+              f32x4{s[cs][t][0], s[cs][t][1], s[cs][t][2], s[cs][t][3]};
+      }
+  };
   // scores of a row in log2 units, and the exponents of its values
-  auto scores = [&](const Row<D>& w, int r, bool on, float (&s)[2][4], int (&ev)[2]) {
+  auto scores = [&](const Row<D>& w, int r, float (&s)[CS][2][4], int (&ev)[2]) {
     const int pos0 = r * kRow;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f};
+      f32x4 a[CS] = {};
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        a = mma<BF16>(widen8<BF16>(w.k[t][c].x, w.k[t][c].y), qf[c][0], a);
-        a = mma<BF16>(widen8<BF16>(w.k[t][c].z, w.k[t][c].w), qf[c][1], a);
+        const u32x4 k0 = widen8<BF16>(w.k[t][c].x, w.k[t][c].y);
+        const u32x4 k1 = widen8<BF16>(w.k[t][c].z, w.k[t][c].w);
+#pragma unroll
+        for (int cs = 0; cs < CS; ++cs) a[cs] = mma<BF16>(k0, qf[cs][c][0], a[cs]);
+#pragma unroll
+        for (int cs = 0; cs < CS; ++cs) a[cs] = mma<BF16>(k1, qf[cs][c][1], a[cs]);
       }
       const float f = scale_log2 * power2(lane_value(w.exps, t) - 127);
       ev[t] = lane_value(w.exps, 2 + t) - 127;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[t][i] = a[i] * f;
+      for (int cs = 0; cs < CS; ++cs)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[cs][t][i] = a[cs][i] * f;
     }
-    if (!on || pos0 + kRow > L - sq + 1) {
-      // positions that a query does not see, slots not written yet (their codes,
-      // a NaN among them, and exponents are not looked at), pages outside the pool
+    if (pos0 + kRow > L - sq + 1) {
+      // positions that a query does not see, and slots not written yet (their codes,
+      // a NaN among them, and exponents are not looked at)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int cs = 0; cs < CS; ++cs)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!on || pos0 + 16 * t + 4 * g + i >= see) s[t][i] = -INFINITY;
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (pos0 + 16 * t + 4 * g + i >= see[cs]) s[cs][t][i] = -INFINITY;
       if (pos0 + 16 >= L) ev[1] = ev[0];
     }
-    if constexpr (SUMS)
-      if (n < ncols) {
-        float* const lg = logits + (((size_t)b * Hkv + kv) * pairs + c0 + n) *
-                                       ((size_t)max_pages * P) + pos0 + 4 * g;
-        *reinterpret_cast<f32x4*>(lg) = f32x4{s[0][0], s[0][1], s[0][2], s[0][3]};
-        *reinterpret_cast<f32x4*>(lg + 16) = f32x4{s[1][0], s[1][1], s[1][2], s[1][3]};
-      }
   };
-  auto rescale = [&](float f) {
+  auto rescale = [&](int cs, float f) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) acc[c][dt] *= f;
+      for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= f;
   };
   // e_ref such that lo .. hi lie in its window
   auto refer = [&](int lo, int hi) {
     e_top = max(e_top, hi);
     if (lo >= e_ref && hi <= e_ref + kRefMax) return;
     const int e = max(max(hi - kRefMax, lo - 4), e_top - kRefFloor);
-    rescale(__builtin_ldexpf(1.0f, e_ref - e));
+    const float f = __builtin_ldexpf(1.0f, e_ref - e);
+#pragma unroll
+    for (int cs = 0; cs < CS; ++cs) rescale(cs, f);
     e_ref = e;
   };
-  // P of a tile in units of 2^(e_ref - ev), its sum into l
-  auto weigh = [&](const float (&s)[4], float mu, int ev, uint32_t (&pf)[2]) {
-    const float by = (float)(ev - e_ref);
-    float p[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = exp2_(s[i] - mu + by);
-    if (ev - e_ref >= -kRefMax) {
-      l = fmaf((p[0] + p[1]) + (p[2] + p[3]), power2(e_ref - ev), l);
-    } else {  // (far below the largest values: P may vanish, l must not)
-      for (int i = 0; i < 4; ++i) l += exp2_(s[i] - mu);
-    }
-    pf[0] = narrow2<false>(p[0], p[1]), pf[1] = narrow2<false>(p[2], p[3]);
-  };
-  auto values = [&](const Row<D>& w, u32x4 pf, uint32_t keep0, uint32_t keep1) {
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        acc[c][dt] = mma<false>(widen8<false>(w.v[0][c][dt] & keep0, w.v[1][c][dt] & keep1), pf,
-                                acc[c][dt]);
-  };
-  auto attend = [&](const Row<D>& w, int r, const float (&s)[2][4], const int (&ev)[2]) {
+  auto attend = [&](Row<D>& w, int r, const float (&s)[CS][2][4], const int (&ev)[2]) {
     const int pos0 = r * kRow;
-    float top = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
-    top = fmaxf(top, fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    if (__any(top > m + kMargin)) {
-      const float mn = fmaxf(m, col_max(top));
-      const float f = m == -INFINITY ? 0.0f : exp2_(m - mn);
-      l *= f;
-      rescale(f);
-      m = mn;
+    float top[CS];
+    bool raise = false;
+#pragma unroll
+    for (int cs = 0; cs < CS; ++cs) {
+      top[cs] = fmaxf(fmaxf(s[cs][0][0], s[cs][0][1]), fmaxf(s[cs][0][2], s[cs][0][3]));
+      top[cs] = fmaxf(top[cs], fmaxf(fmaxf(s[cs][1][0], s[cs][1][1]), fmaxf(s[cs][1][2], s[cs][1][3])));
+      raise |= top[cs] > m[cs] + kMargin;
     }
-    const float mu = m == -INFINITY ? 0.0f : m;
-    uint32_t keep0 = 0xffffffffu, keep1 = 0xffffffffu;
-    if (pos0 + kRow > L) {
-      const int a = min(max(L - pos0 - 4 * g, 0), 4), c = min(max(L - pos0 - 16 - 4 * g, 0), 4);
-      keep0 = a ? 0xffffffffu >> (8 * (4 - a)) : 0u;
-      keep1 = c ? 0xffffffffu >> (8 * (4 - c)) : 0u;
+    if (__any(raise)) {
+#pragma unroll
+      for (int cs = 0; cs < CS; ++cs) {
+        const float mn = fmaxf(m[cs], col_max(top[cs]));
+        const float f = m[cs] == -INFINITY ? 0.0f : exp2_(m[cs] - mn);
+        l[cs] *= f;
+        rescale(cs, f);
+        m[cs] = mn;
+      }
     }
-    const int lo = min(ev[0], ev[1]), hi = max(ev[0], ev[1]);
-    uint32_t p0[2], p1[2];
-    if (hi - lo <= kRefMax) {
+    if (pos0 + kRow > L) {  // slots not written yet: zeros (their codes may be NaN)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int a = min(max(L - pos0 - 16 * t - 4 * g, 0), 4);
+        const uint32_t keep = a ? 0xffffffffu >> (8 * (4 - a)) : 0u;
+#pragma unroll
+        for (int c = 0; c < C; ++c) w.v[t][c] &= keep;
+      }
+    }
+    // both tiles with one reference, or one after the other where their exponents
+    // are too far apart for that
+    int lo = min(ev[0], ev[1]), hi = max(ev[0], ev[1]);
+    const int parts = hi - lo <= kRefMax ? 1 : 2;
+    for (int part = 0; part < parts; ++part) {
+      if (parts > 1) lo = hi = part ? ev[1] : ev[0];
       refer(lo, hi);
-      weigh(s[0], mu, ev[0], p0);
-      weigh(s[1], mu, ev[1], p1);
-      values(w, u32x4{p0[0], p0[1], p1[0], p1[1]}, keep0, keep1);
-    } else {  // too far apart for one reference: tile by tile
-      refer(ev[0], ev[0]);
-      weigh(s[0], mu, ev[0], p0);
-      values(w, u32x4{p0[0], p0[1], 0u, 0u}, keep0, 0u);
-      refer(ev[1], ev[1]);
-      weigh(s[1], mu, ev[1], p1);
-      values(w, u32x4{0u, 0u, p1[0], p1[1]}, 0u, keep1);
+      u32x4 pf[CS];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bool here = parts == 1 || part == t;
+        const float by = (float)(ev[t] - e_ref);
+#pragma unroll
+        for (int cs = 0; cs < CS; ++cs) {
+          const float mu = m[cs] == -INFINITY ? 0.0f : m[cs];
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = exp2_(s[cs][t][i] - mu + by);
+          if (here) {
+            if (ev[t] - e_ref >= -kRefMax) {
+              l[cs] = fmaf((p[0] + p[1]) + (p[2] + p[3]), power2(e_ref - ev[t]), l[cs]);
+            } else {  // (far below the largest values: P may vanish, l must not)
+              for (int i = 0; i < 4; ++i) l[cs] += exp2_(s[cs][t][i] - mu);
+            }
+          }
+          pf[cs][2 * t] = here ? narrow2<false>(p[0], p[1]) : 0u;
+          pf[cs][2 * t + 1] = here ? narrow2<false>(p[2], p[3]) : 0u;
+        }
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) {
+          // (opaque: widened ahead of the loop over the parts, all operands would
+          // be held at once)
+          uint32_t v0 = w.v[0][c][dt], v1 = w.v[1][c][dt];
+          asm volatile("" : "+v"(v0), "+v"(v1));
+          const u32x4 a = widen8<false>(v0, v1);
+#pragma unroll
+          for (int cs = 0; cs < CS; ++cs) acc[cs][c][dt] = mma<false>(a, pf[cs], acc[cs][c][dt]);
+        }
     }
   };
 
   if (r0 < r1) {
-    constexpr int NB = D > 128 ? 1 : 2;
+    // NB rows in flight.  One is enough: four waves then keep 32 KB (at d = 128) on
+    // the way per CU, and three blocks fit on one; two took 86.9 against 85.2 us at
+    // 262,144 positions and 80 against 70 for eight requests of 20,000.
+    constexpr int NB = 1;
     Row<D> w[NB];
     int pid[NB], ahead[NB];
 #pragma unroll
@@ -270,9 +316,18 @@ __global__ __launch_bounds__(kThreads) void kv8_decode_kernel(
       for (int i = 0; i < NB; ++i) {
         const int r = rr + i * kWaves, rn = r + NB * kWaves;
         const bool on = (uint32_t)pid[i] < (uint32_t)num_pages;
-        float s[2][4];
+        float s[CS][2][4];
         int ev[2];
-        if (r < r1) scores(w[i], r, on, s, ev);
+        if (r < r1) {
+          scores(w[i], r, s, ev);
+          if (!on) {
+#pragma unroll
+            for (int cs = 0; cs < CS; ++cs)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) s[cs][e / 4][e % 4] = -INFINITY;
+          }
+          if (SUMS) keep_scores(r, s);
+        }
         fetch_k(w[i], rn, ahead[i]);
         if (r < r1 && on) attend(w[i], r, s, ev);
         fetch_v(w[i], rn, ahead[i]);
@@ -283,22 +338,35 @@ __global__ __launch_bounds__(kThreads) void kv8_decode_kernel(
   }
 
   // ---- merge the waves in LDS: o (units 1), m, l of the block's columns
-  l = col_sum(l);
-  {
-    float* part = smem + (size_t)(wave * ncols + n) * kPart;
-    if (n < ncols) {
+#pragma unroll
+  for (int cs = 0; cs < CS; ++cs) {
+    const float den = col_sum(l[cs]);
+    const int col = kCols * cs + n;
+    float* part = smem + (size_t)(wave * ncols + col) * kPart;
+    if (col < ncols) {
       const float f = __builtin_ldexpf(1.0f, e_ref);
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           *reinterpret_cast<f32x4*>(part + 64 * c + 16 * g + 4 * i) =
-              f32x4{acc[c][0][i], acc[c][1][i], acc[c][2][i], acc[c][3][i]} * f;
-      if (g == 0) part[D] = m, part[D + 1] = l;
+              f32x4{acc[cs][c][0][i], acc[cs][c][1][i], acc[cs][c][2][i], acc[cs][c][3][i]} * f;
+      if (g == 0) part[D] = m[cs], part[D + 1] = den;
     }
   }
   __syncthreads();
   const size_t rec0 = ((size_t)b * Hkv + kv) * pairs + c0;  // the block's first (request, pair)
+  // the block's records, written and read with device-scope coherent accesses
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+      recs + rec0 * max_splits * kPart, (short)0, (int)(ncols * max_splits * kPart * 4), 0x00020000);
+  constexpr int kSc1 = 16;
+  auto store_rec = [&](int col, int at, int d4, int ml0, f32x4 o, float M, float den) {
+    const int rec = (col * max_splits + at) * kPart * 4;
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rs, rec + 16 * d4, 0, kSc1);
+    if (d4 == 0)
+      __builtin_amdgcn_raw_buffer_store_b64(
+          __builtin_bit_cast(u32x2, f32x2{M, den}), rs, rec + 4 * (D + ml0), 0, kSc1);
+  };
   auto store_out = [&](int col, int d4, f32x4 o) {
     const int pr = c0 + col;
     uint16_t* op = out + (((size_t)b * sq + pr / gq) * Hq + kv * gq + pr % gq) * D + 4 * d4;
@@ -324,71 +392,108 @@ __global__ __launch_bounds__(kThreads) void kv8_decode_kernel(
       store_out(col, d4, num * (den > 0.0f ? 1.0f / den : 0.0f));
       if (SUMS && d4 == 0) lse[rec0 + col] = den > 0.0f ? M + log2f(den) : INFINITY;
     } else {
-      // agent-scope stores: written through to the device-coherent level, where
-      // the block that combines (on any XCD) reads them
-      float* rec = recs + ((rec0 + col) * max_splits + split) * kPart;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        __hip_atomic_store(rec + 4 * d4 + e, num[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (d4 == 0) {
-        __hip_atomic_store(rec + D, M, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __hip_atomic_store(rec + D + 1, den, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
+      store_rec(col, split, d4, 0, num, M, den);
     }
   }
   if (S == 1) return;
 
-  // ---- the last split to finish combines the records.  Every word the blocks
-  // exchange is written and read by device-scope atomic instructions; each
-  // thread waits for its record stores before the barrier that precedes the
-  // ticket, and the combining block loads records only after it has seen the
-  // last ticket (the decode over 4-bit pages argues this exchange in full).
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  uint32_t* const ticket = tickets + ((size_t)b * Hkv + kv) * n_hchunks + hc;
+  // ---- the last split to finish combines the records; where they are many, the
+  // last of each group of splits first joins the group's (into its first record,
+  // m and l behind the split's own).  Every word the blocks exchange is written
+  // and read by device-scope coherent accesses (sc1: written through to, and read
+  // from, the level that all XCDs share); each thread waits for its
+  // record stores before the barrier that precedes the ticket, and the combining
+  // block loads records only after it has seen the last ticket (the decode over
+  // 4-bit pages argues this exchange in full).
   uint32_t* const s_ticket = reinterpret_cast<uint32_t*>(smem);
-  if (tid == 0)
-    *s_ticket = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (*s_ticket != (uint32_t)(S - 1)) return;
-  if (tid == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  auto load = [&](const float* p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  };
-  for (int i = tid; i < ncols * (D / 4); i += kThreads) {
-    const int col = i / (D / 4), d4 = i % (D / 4);
-    const float* rec = recs + (rec0 + col) * max_splits * kPart;
-    float M = -INFINITY, den = 0.0f;
-    f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
-    constexpr int kAt = 8;  // records in flight
-    for (int s0 = 0; s0 < S; s0 += kAt) {
-      f32x4 o[kAt];
-      float ms[kAt], ls[kAt];
-#pragma unroll
-      for (int k = 0; k < kAt; ++k) {
-        const float* rs = rec + (size_t)min(s0 + k, S - 1) * kPart;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[k][e] = load(rs + 4 * d4 + e);
-        ms[k] = load(rs + D), ls[k] = load(rs + D + 1);
-      }
-      float mx = M;
-#pragma unroll
-      for (int k = 0; k < kAt; ++k) {
-        if (s0 + k >= S) ms[k] = -INFINITY;
-        mx = fmaxf(mx, ms[k]);
-      }
-      const float f = M == -INFINITY ? 0.0f : exp2_(M - mx);
-      num *= f, den *= f, M = mx;
-#pragma unroll
-      for (int k = 0; k < kAt; ++k) {
-        const float fk = ms[k] == -INFINITY ? 0.0f : exp2_(ms[k] - M);
-        num += o[k] * fk;
-        den = fmaf(fk, ls[k], den);
-      }
+  auto last_of = [&](uint32_t* ticket, int count) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+      const uint32_t t = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (t == (uint32_t)(count - 1))
+        __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *s_ticket = t;
     }
+    __syncthreads();
+    return *s_ticket == (uint32_t)(count - 1);
+  };
+  // Joins `count` records from `first` on, `step` apart, whose m and l lie at
+  // float D + ml; done(col, d4, num, den, M) gets the sums of four dims.  GR
+  // groups of threads share the records, kAt in flight each, and meet in LDS.
+  const int items = ncols * (D / 4), GR = min(max(kThreads / items, 1), 8);
+  f32x4* const s_num = reinterpret_cast<f32x4*>(smem) + 1;
+  float* const s_ml = reinterpret_cast<float*>(s_num + kThreads);
+  auto join = [&](int first, int count, int step, int ml0, auto&& done) {
+    constexpr int kAt = 8;
+    for (int i0 = 0; i0 < items; i0 += kThreads) {  // (one turn where GR > 1)
+      const int i = GR > 1 ? tid % items : i0 + tid, gr = GR > 1 ? tid / items : 0;
+      const bool on = i < items && gr < GR;
+      const int col = min(i, items - 1) / (D / 4), d4 = i % (D / 4);
+      float M = -INFINITY, den = 0.0f;
+      f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (on)
+        for (int s0 = gr; s0 < count; s0 += GR * kAt) {
+          f32x4 o[kAt];
+          f32x2 ml[kAt];
+#pragma unroll
+          for (int k = 0; k < kAt; ++k) {
+            const int at = (col * max_splits + first + min(s0 + k * GR, count - 1) * step) * kPart * 4;
+            o[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16 * d4, 0, kSc1));
+            ml[k] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, at + 4 * (D + ml0), 0, kSc1));
+          }
+          float mx = M;
+#pragma unroll
+          for (int k = 0; k < kAt; ++k) {
+            if (s0 + k * GR >= count) ml[k].x = -INFINITY;
+            mx = fmaxf(mx, ml[k].x);
+          }
+          const float f = M == -INFINITY ? 0.0f : exp2_(M - mx);
+          num *= f, den *= f, M = mx;
+#pragma unroll
+          for (int k = 0; k < kAt; ++k) {
+            const float fk = ml[k].x == -INFINITY ? 0.0f : exp2_(ml[k].x - M);
+            num += o[k] * fk;
+            den = fmaf(fk, ml[k].y, den);
+          }
+        }
+      if (GR > 1) {
+        s_num[tid] = num, s_ml[2 * tid] = M, s_ml[2 * tid + 1] = den;
+        __syncthreads();
+        if (gr == 0) {
+          for (int k = 1; k < GR; ++k) {
+            const int o = tid + k * items;
+            const float mo = s_ml[2 * o], mx = fmaxf(M, mo);
+            const float fa = M == -INFINITY ? 0.0f : exp2_(M - mx);
+            const float fb = mo == -INFINITY ? 0.0f : exp2_(mo - mx);
+            num = num * fa + s_num[o] * fb;
+            den = den * fa + s_ml[2 * o + 1] * fb;
+            M = mx;
+          }
+        }
+      }
+      if (on && gr == 0) done(col, d4, num, den, M);
+      if (GR > 1) break;
+    }
+  };
+  auto finish = [&](int col, int d4, f32x4 num, float den, float M) {
     store_out(col, d4, num * (den > 0.0f ? 1.0f / den : 0.0f));
     if (SUMS && d4 == 0) lse[rec0 + col] = den > 0.0f ? M + log2f(den) : INFINITY;
+  };
+  const size_t unit = ((size_t)b * Hkv + kv) * n_hchunks + hc;
+  // (a split that exceeds max_splits / group_splits groups does not exist)
+  const int GS = group_splits;
+  if (GS == 0 || S <= GS) {
+    if (last_of(tickets + unit * (GS ? kGroups + 1 : 1), S)) join(0, S, 1, 0, finish);
+    return;
   }
+  const int grp = split / GS, groups = (S + GS - 1) / GS;
+  uint32_t* const mine = tickets + unit * (kGroups + 1);
+  if (!last_of(mine + 1 + grp, min(GS, S - grp * GS))) return;
+  join(grp * GS, min(GS, S - grp * GS), 1, 0, [&](int col, int d4, f32x4 num, float den, float M) {
+    store_rec(col, grp * GS, d4, 2, num, M, den);
+  });
+  if (last_of(mine, groups)) join(0, groups, GS, 2, finish);
 }
 
 // weights[b][kv][t] += sum over the pairs of exp2(s_t - lse): the decode left
@@ -418,27 +523,38 @@ __global__ __launch_bounds__(256) void kv8_sums_kernel(const float* __restrict__
     if (t + e < L) w[e] += sum[e];
 }
 
-template <int D, bool BF16, bool SUMS>
-hipError_t launch(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q, int32_t B,
+template <int D, bool BF16, bool SUMS, int CS>
+hipError_t launch_cs(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q, int32_t B,
                   int32_t sq, int32_t Hq, const int32_t* bt, int32_t max_pages, const int32_t* lens,
                   float scale, int32_t max_splits, void* ws, void* out, float* weights,
                   int64_t stride, hipStream_t stream) {
   const int Hkv = L.num_kv_heads, pairs = Hq / Hkv * sq;
-  const int n_hchunks = (pairs + kCols - 1) / kCols;
+  const int n_hchunks = (pairs + kCols * CS - 1) / (kCols * CS);
   // enough blocks for one per CU when one request runs alone; the count
   // depends on neither the batch nor the lengths, so that a request's output
   // is bitwise the same in any batch
   const int split_cap = (int)std::max<int64_t>(
       1, std::min<int64_t>(max_splits, num_cus() / ((int64_t)Hkv * n_hchunks)));
   const int64_t slots = ((int64_t)split_cap * Hkv + kXcds - 1) / kXcds * kXcds;
+  // Joining the records takes one block a round trip per eight of them, for each
+  // 1,024 floats of its columns; from five on, groups of splits are joined first
+  // (if there are counters for them).
+  const int64_t floats = (int64_t)std::min(kCols * CS, pairs) * D, turns = (floats + 4 * kThreads - 1) / (4 * kThreads);
+  const int64_t rounds = turns * ((split_cap + 7) / 8) / std::max<int64_t>(1, 4 * kThreads / floats);
+  const int64_t units = (int64_t)B * Hkv * n_hchunks;
+  int group_splits = 0;
+  if (rounds >= 5 && units * (kGroups + 1) <= kDecodeMaxHeads)
+    group_splits = std::max(8, (split_cap + kGroups - 1) / kGroups);
   const Kv8Workspace at = kv8_workspace(B, sq, Hq, D, max_splits, SUMS ? max_pages * L.page_size : 0);
   uint8_t* base = static_cast<uint8_t*>(ws);
   float* lse = reinterpret_cast<float*>(base + at.lse);
   float* logits = reinterpret_cast<float*>(base + at.logits);
   int shift = 0;
   while ((1 << shift) < L.group_size) ++shift;
-  const size_t lds = sizeof(float) * kWaves * std::min(kCols, pairs) * (D + 4);
-  const auto kernel = kv8_decode_kernel<D, BF16, SUMS>;
+  // the waves' partials; then the ticket and the combine's parts
+  const size_t lds = std::max<size_t>(sizeof(float) * kWaves * std::min(kCols * CS, pairs) * (D + 4),
+                                      16 + kThreads * 24);
+  const auto kernel = kv8_decode_kernel<D, BF16, SUMS, CS>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -452,13 +568,24 @@ hipError_t launch(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void
                      lens, reinterpret_cast<uint32_t*>(base),
                      reinterpret_cast<float*>(base + at.records), lse, logits,
                      static_cast<uint16_t*>(out), Hq, sq, Hkv, L.page_size, shift, L.num_pages,
-                     max_pages, max_splits, split_cap, n_hchunks, scale * 1.44269504088896340736f);
+                     max_pages, max_splits, split_cap, n_hchunks, group_splits, scale * 1.44269504088896340736f);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !SUMS) return e;
   const int cap = max_pages * L.page_size;
   hipLaunchKernelGGL(kv8_sums_kernel, dim3((uint32_t)((cap + 1023) / 1024), Hkv, B), dim3(256), 0,
                      stream, logits, lse, lens, weights, stride, pairs, cap);
   return hipGetLastError();
+}
+
+template <int D, bool BF16, bool SUMS>
+hipError_t launch(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q, int32_t B,
+                  int32_t sq, int32_t Hq, const int32_t* bt, int32_t max_pages, const int32_t* lens,
+                  float scale, int32_t max_splits, void* ws, void* out, float* weights,
+                  int64_t stride, hipStream_t stream) {
+  const auto go = Hq / L.num_kv_heads * sq > kCols ? launch_cs<D, BF16, SUMS, 2>
+                                                   : launch_cs<D, BF16, SUMS, 1>;
+  return go(L, pool, q, B, sq, Hq, bt, max_pages, lens, scale, max_splits, ws, out, weights, stride,
+            stream);
 }
 
 }  // namespace
