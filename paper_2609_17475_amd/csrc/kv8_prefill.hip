@@ -5,14 +5,16 @@
 //   s_it = scale * q_i . k_t  (t <= prefix + i),  lse_i = log sum_t exp(s_it)
 //   o_i = sum_t exp(s_it - lse_i) v_t,  w_t += sum_i exp(s_it - lse_i)
 //
-// Bound by the matrix cores and the vector work beside them (an exponential
-// and four more instructions per score, one conversion per two codes).  The
+// Bound by the matrix cores and the vector work beside them (an exponential and
+// three more instructions per score): a SIMD's vector instructions take ~4.7
+// cycles each and every matrix product holds up another 6-8.  The
 // (row, head) pairs that read a KV head are the columns of the products, as in
 // kv8_decode.hip, whose operand layouts and exponents' handling are the same.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "jfkv_internal.h"
 #include "jfkv_kv8.h"
@@ -21,6 +23,8 @@ namespace jfkv {
 namespace {
 
 using namespace kv8;
+
+#define JF_INLINE __attribute__((always_inline))
 
 constexpr int kTile = 64;        // positions of a tile (in one page)
 constexpr int kWaves = 8;
@@ -62,10 +66,10 @@ __device__ __forceinline__ void load_q(u32x4 (&qf)[C][2], const uint16_t* qp, in
 }
 
 // One block: block_cols columns of one KV head, the tiles of one split.  A tile's
-// K and V codes are fetched two tiles ahead into registers, go to LDS in
-// operand order one tile ahead (K: [16 positions][64 dims][lane][16 B]; V as it
-// lies), and are widened by each wave as it uses them.  SPLIT: fp32 partials
-// (o, m, l) to ws [split][Hkv][columns][D + 4] instead of rows.
+// K and V codes are fetched into registers two tiles ahead, widened once for the
+// block and laid into LDS as the matrix operands that all waves read.  Several
+// splits: fp32 partials (o, m, l) to ws [split][Hkv][columns][D + 4] instead of
+// rows.
 template <int D, bool BF16>
 __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
@@ -74,8 +78,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
     uint16_t* __restrict__ out, float* __restrict__ lse, int Hq, int Hkv, int P, int block_shift,
     int num_pages, int T, int prefix, int n_rb, int n_split, float scale_log2, uint32_t flip) {
   constexpr int C = D / 64, NC = col_sets<D>(), COLS = block_cols<D>();
-  constexpr int kItems = 128 * D / 16 / kThreads;  // 16-byte pieces of a tile per thread
-  __shared__ __align__(16) u32x4 tiles[2][8 * D];  // K, then V
+  __shared__ __align__(16) u32x4 tiles_k[2][8 * D], tiles_v[2][8 * D];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // KV head fastest (one XCD's L2 sees few heads), the longest row blocks first
@@ -109,85 +112,136 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
   for (int cs = 0; cs < NC; ++cs) m[cs] = -INFINITY, l[cs] = 0.0f;
   int e_ref = 0, e_top = -1000;
 
-  // ---- tile transport
-  u32x4 stage[kItems];
-  uint32_t exps_next = 0, exps = 0;  // lanes 0..3: K's exponent bytes of the tile, 4..7: V's
-  auto page_of = [&](int j) { return table[min(j, j1 - 1) * kTile / P]; };
-  auto fetch = [&](int j, int pid) {
-    const int slot0 = min(j, j1 - 1) * kTile % P;
-    const size_t run = (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv;
+  // ---- tile transport: K's codes are fetched two tiles ahead and go to LDS one
+  // tile ahead, V's one tile later each
+  constexpr int kPieces = 4 * D / kThreads > 0 ? 4 * D / kThreads : 1;  // of 16 bytes per thread
+  constexpr int kOf = 4 * D < kThreads ? 4 * D : kThreads;              // threads that take some
+  u32x4 k_stage[kPieces], v_stage[kPieces];
+  uint32_t exps = 0, exps_next = 0;  // lanes 0..3: K's exponent bytes of a tile, 4..7: V's
+  // the place of a tile, stepped without divisions
+  struct Place {
+    int page, slot;
+  };
+  const int last_page = (j1 * kTile - 1) / P;
+  auto step = [&](Place& at) JF_INLINE {
+    at.slot += kTile;
+    if (at.slot == P) at.slot = 0, ++at.page;
+  };
+  auto page_of = [&](const Place& at) JF_INLINE { return table[min(at.page, last_page)]; };
+  auto run_of = [&](int pid) JF_INLINE { return (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv; };
+  const uint32_t k_off = (tid / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
+  auto fetch_k = [&](int slot0, int pid) JF_INLINE {
+    const size_t run = run_of(pid);
     const uint8_t* kp = k_codes + (run * P + slot0) * D;
-    const uint8_t* vp = v_codes + (run * P + slot0) * D;
+    if (kOf == kThreads || tid < kOf) {
 #pragma unroll
-    for (int k = 0; k < kItems; ++k) {
-      const int i = tid + k * kThreads;
-      if (i < 4 * D) {
-        const int r = i % D, ln = r & 63;
-        stage[k] = *reinterpret_cast<const u32x4*>(kp + ((i / D) * 16 + (ln & 15)) * D +
-                                                    (r >> 6) * 64 + (ln >> 4) * 16);
-      } else {
-        stage[k] = *reinterpret_cast<const u32x4*>(vp + (i - 4 * D) * 16);
-      }
+      for (int k = 0; k < kPieces; ++k)
+        k_stage[k] = *reinterpret_cast<const u32x4*>(kp + k_off + k * (kThreads / D) * 16 * D);
     }
     const uint8_t* ep = (lane & 4) ? v_exps : k_exps;
     exps_next = ep[run * (P >> block_shift) + ((slot0 + 16 * (lane & 3)) >> block_shift)];
   };
-  auto deposit = [&](int j) {
-    if ((j + 1) * kTile > L) {
-      // slots not written yet: zeros for their values (their codes may be NaN)
+  auto fetch_v = [&](int slot0, int pid) JF_INLINE {
+    const uint8_t* vp = v_codes + (run_of(pid) * P + slot0) * D;
+    if (kOf == kThreads || tid < kOf) {
 #pragma unroll
-      for (int k = 0; k < kItems; ++k) {
-        const int i = tid + k * kThreads - 4 * D;
-        if (i >= 0) {
-          const int left = min(max(L - (j * kTile + (i / D) * 16 + (i % 64) / 16 * 4), 0), 4);
-          stage[k] &= left ? 0xffffffffu >> (8 * (4 - left)) : 0u;
-        }
+      for (int k = 0; k < kPieces; ++k)
+        v_stage[k] = *reinterpret_cast<const u32x4*>(vp + (tid + k * kThreads) * 16);
+    }
+  };
+  auto deposit_k = [&](int j) JF_INLINE {
+    if (kOf < kThreads && tid >= kOf) return;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int i = tid + k * kThreads;
+      // [16 positions][64 dims][half][lane]
+      u32x4* to = tiles_k[j & 1] + i / 64 * 128 + i % 64;
+      to[0] = widen8<BF16>(k_stage[k].x, k_stage[k].y), to[64] = widen8<BF16>(k_stage[k].z, k_stage[k].w);
+    }
+  };
+  auto deposit_v = [&](int j) JF_INLINE {
+    if (kOf < kThreads && tid >= kOf) return;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int i = tid + k * kThreads;
+      if ((j + 1) * kTile > L) {  // slots not written yet: zeros (their codes may be NaN)
+        const int left = min(max(L - (j * kTile + i / D * 16 + i % 64 / 16 * 4), 0), 4);
+        v_stage[k] &= left ? 0xffffffffu >> (8 * (4 - left)) : 0u;
+      }
+      // [32 positions][64 dims][dim % 4][lane][16 of the 32]
+      u32x2* to = reinterpret_cast<u32x2*>(tiles_v[j & 1] + (i / D / 2 * C + i % D / 64) * 256 + i % 64) + i / D % 2;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        uint32_t lo, hi;
+        widen<false>(v_stage[k][dt], lo, hi);
+        to[dt * 128] = u32x2{lo, hi};
       }
     }
-#pragma unroll
-    for (int k = 0; k < kItems; ++k) tiles[j & 1][tid + k * kThreads] = stage[k];
   };
 
-  auto rescale = [&](int cs, float f) {
+  auto rescale = [&](float f) JF_INLINE {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int cs = 0; cs < NC; ++cs)
 #pragma unroll
-      for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= f;
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= f;
   };
 
-  auto compute = [&](int j) {
-    const u32x4* kt = tiles[j & 1];
-    const u32x4* vt = kt + 4 * D;
-    const int pos0 = j * kTile;
-    // scores, times f[t] in log2 units
-    f32x4 s[4][NC];
-    float f[4];
-    int ev[4];
+  // ---- a tile's three steps: scores (matrix cores), softmax (vector), values
+  // (matrix cores)
+  f32x4 s[4][NC];      // scores, times f[t] in log2 units
+  float f[4];
+  int ev[4];           // the values' exponents
+  uint32_t pf[2][NC][4];  // P as B operands
+  int split_e[4];      // where apart: the references of the tile's parts
+  bool apart = false;
+
+  // A run of operands that lie one after the other in LDS, each read kAhead
+  // before its products.  (The barriers keep the compiler from reading all of
+  // them at once, which spills.)
+  constexpr int kAhead = 4;
+  auto stream = [&](const u32x4* from, auto first, auto count, auto&& use) JF_INLINE {
+    constexpr int n0 = decltype(first)::value, nn = decltype(count)::value;
+    u32x4 ring[kAhead];
+#pragma unroll
+    for (int p = 0; p < kAhead; ++p) ring[p] = from[(n0 + p) * 64 + lane];
+#pragma unroll
+    for (int p = 0; p < nn; ++p) {
+      const u32x4 a = ring[p % kAhead];
+      if (p + kAhead < nn) ring[p % kAhead] = from[(n0 + p + kAhead) * 64 + lane];
+      use(n0 + p, a);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  auto scores = [&](int j) JF_INLINE {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
       for (int cs = 0; cs < NC; ++cs) s[t][cs] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const u32x4 kc = kt[t * D + c * 64 + lane];
-        const u32x4 a0 = widen8<BF16>(kc.x, kc.y), a1 = widen8<BF16>(kc.z, kc.w);
-#pragma unroll
-        for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a0, qf[cs][c][0], s[t][cs]);
-#pragma unroll
-        for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a1, qf[cs][c][1], s[t][cs]);
-      }
       // (not 0, so that a hidden score times it stays -inf)
       f[t] = fmaxf(scale_log2 * power2(__builtin_amdgcn_readlane((int)exps, t) - 127), 1e-37f);
       ev[t] = __builtin_amdgcn_readlane((int)exps, 4 + t) - 127;
     }
-    if (pos0 + kTile - 1 > prefix + w_lo) {
+    stream(tiles_k[j & 1], std::integral_constant<int, 0>{}, std::integral_constant<int, 8 * C>{},
+           [&](int p, u32x4 a) JF_INLINE {
+             const int t = p / (2 * C), c = p / 2 % C, half = p % 2;
+#pragma unroll
+             for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a, qf[cs][c][half], s[t][cs]);
+           });
+  };
+
+  auto softmax = [&](int j, bool on) JF_INLINE {
+    const int pos0 = j * kTile;
+    if (!on || pos0 + kTile - 1 > prefix + w_lo) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
 #pragma unroll
         for (int cs = 0; cs < NC; ++cs)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (pos0 + 16 * t + 4 * g + i > prefix + row[cs]) s[t][cs][i] = -INFINITY;
+            if (!on || pos0 + 16 * t + 4 * g + i > prefix + row[cs]) s[t][cs][i] = -INFINITY;
         if (pos0 + 16 * t >= L) f[t] = 1.0f, ev[t] = ev[0];  // (exponents not written yet)
       }
     }
@@ -209,81 +263,159 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
         const float mn = fmaxf(m[cs], col_max(top[cs]));
         const float by = m[cs] == -INFINITY ? 0.0f : exp2_(m[cs] - mn);
         l[cs] *= by;
-        rescale(cs, by);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= by;
         m[cs] = mn;
       }
     }
-    // the values' exponents: one reference for the tile, or one part per 16
-    // positions where they are too far apart for that
+    float mu[NC];
+#pragma unroll
+    for (int cs = 0; cs < NC; ++cs) mu[cs] = m[cs] == -INFINITY ? 0.0f : m[cs];
     int lo = ev[0], hi = ev[0];
 #pragma unroll
     for (int t = 1; t < 4; ++t) lo = min(lo, ev[t]), hi = max(hi, ev[t]);
-    const int parts = hi - lo <= kRefMax ? 1 : 4;
-    for (int part = 0; part < parts; ++part) {
-      if (parts > 1) lo = hi = part == 0 ? ev[0] : part == 1 ? ev[1] : part == 2 ? ev[2] : ev[3];
-      e_top = max(e_top, hi);
+    e_top = max(e_top, hi);
+    apart = hi - lo > kRefMax || lo < e_top - kRefFloor;
+    if (!apart) {
+      // one reference for the tile's values
       if (lo < e_ref || hi > e_ref + kRefMax) {
-        const int e = max(max(hi - kRefMax, lo - 4), e_top - kRefFloor);
-        const float by = __builtin_ldexpf(1.0f, e_ref - e);
-#pragma unroll
-        for (int cs = 0; cs < NC; ++cs) rescale(cs, by);
+        const int e = max(hi - kRefMax, lo - 4);
+        rescale(__builtin_ldexpf(1.0f, e_ref - e));
         e_ref = e;
       }
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        u32x4 pf[NC];
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const int t = 2 * t2 + u;
-          const bool on = parts == 1 || part == t;
-          const float by = (float)(ev[t] - e_ref);
+        for (int cs = 0; cs < NC; ++cs) {
+          const float by = (float)(ev[t] - e_ref) - mu[cs];
+          float p[4];
 #pragma unroll
-          for (int cs = 0; cs < NC; ++cs) {
-            const float mu = m[cs] == -INFINITY ? 0.0f : m[cs];
-            float p[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = exp2_(fmaf(s[t][cs][i], f[t], by - mu));
-            if (on) {
-              if (ev[t] - e_ref >= -kRefMax) {
-                l[cs] = fmaf((p[0] + p[1]) + (p[2] + p[3]), power2(e_ref - ev[t]), l[cs]);
-              } else {  // (far below the largest values: P may vanish, l must not)
-                for (int i = 0; i < 4; ++i) l[cs] += exp2_(fmaf(s[t][cs][i], f[t], -mu));
-              }
-            }
-            pf[cs][2 * u] = on ? narrow2<false>(p[0], p[1]) : 0u;
-            pf[cs][2 * u + 1] = on ? narrow2<false>(p[2], p[3]) : 0u;
-          }
+          for (int i = 0; i < 4; ++i) p[i] = exp2_(fmaf(s[t][cs][i], f[t], by));
+          l[cs] = fmaf((p[0] + p[1]) + (p[2] + p[3]), power2(e_ref - ev[t]), l[cs]);
+          pf[t / 2][cs][t % 2 * 2] = narrow2<false>(p[0], p[1]);
+          pf[t / 2][cs][t % 2 * 2 + 1] = narrow2<false>(p[2], p[3]);
         }
+    } else {
+      // too far apart for that (or far below the largest values, where P may
+      // vanish and l must not): a reference for each 16 positions
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const u32x4 v0 = vt[2 * t2 * D + c * 64 + lane], v1 = vt[(2 * t2 + 1) * D + c * 64 + lane];
+      for (int t = 0; t < 4; ++t) {
+        split_e[t] = max(ev[t] - 4, e_top - kRefFloor);
 #pragma unroll
-          for (int dt = 0; dt < 4; ++dt) {
-            const u32x4 a = widen8<false>(v0[dt], v1[dt]);
+        for (int cs = 0; cs < NC; ++cs) {
+          const float by = (float)(ev[t] - split_e[t]) - mu[cs];
+          float p[4];
 #pragma unroll
-            for (int cs = 0; cs < NC; ++cs) acc[cs][c][dt] = mma<false>(a, pf[cs], acc[cs][c][dt]);
+          for (int i = 0; i < 4; ++i) {
+            const float x = s[t][cs][i] * f[t];
+            p[i] = exp2_(x + by);
+            l[cs] += exp2_(x - mu[cs]);
           }
+          pf[t / 2][cs][t % 2 * 2] = narrow2<false>(p[0], p[1]);
+          pf[t / 2][cs][t % 2 * 2 + 1] = narrow2<false>(p[2], p[3]);
         }
       }
     }
   };
 
-  if (j0 < j1) {
-    int pid = page_of(j0), pid1 = page_of(j0 + 1), pid2 = page_of(j0 + 2);
-    fetch(j0, pid);
-    exps = exps_next;
-    deposit(j0);
-    fetch(j0 + 1, pid1);
-    for (int j = j0; j < j1; ++j) {
-      __syncthreads();  // tile j is in LDS, tile j - 1 is done with
-      const uint32_t exps_1 = exps_next;
-      if (j + 1 < j1) deposit(j + 1);
-      fetch(j + 2, pid2);
-      const int pid3 = page_of(j + 3);
-      if (active && (uint32_t)pid < (uint32_t)num_pages && j * kTile <= prefix + w_hi) compute(j);
-      exps = exps_1;
-      pid = pid1, pid1 = pid2, pid2 = pid3;
+  auto values = [&](int j) JF_INLINE {
+    auto products = [&](auto t2, const u32x4 (&b)[NC]) {
+      stream(tiles_v[j & 1], std::integral_constant<int, decltype(t2)::value * 4 * C>{},
+             std::integral_constant<int, 4 * C>{}, [&](int p, u32x4 a) JF_INLINE {
+               const int c = p / 4 % C, dt = p % 4;
+#pragma unroll
+               for (int cs = 0; cs < NC; ++cs) acc[cs][c][dt] = mma<false>(a, b[cs], acc[cs][c][dt]);
+             });
+    };
+    constexpr std::integral_constant<int, 0> t0{};
+    constexpr std::integral_constant<int, 1> t1{};
+    if (!apart) {
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        u32x4 b[NC];
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) b[cs] = u32x4{pf[t2][cs][0], pf[t2][cs][1], pf[t2][cs][2], pf[t2][cs][3]};
+        if (t2 == 0) products(t0, b); else products(t1, b);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        rescale(__builtin_ldexpf(1.0f, e_ref - split_e[t]));
+        e_ref = split_e[t];
+        u32x4 b[NC];
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs)
+          b[cs] = t % 2 ? u32x4{0u, 0u, pf[t / 2][cs][2], pf[t / 2][cs][3]}
+                        : u32x4{pf[t / 2][cs][0], pf[t / 2][cs][1], 0u, 0u};
+        if (t < 2) products(t0, b); else products(t1, b);
+      }
     }
+  };
+
+  // ---- Turn j forms the scores of tile j and the value products of tile j - 1.
+  // Waves w and w + 4 share a SIMD: the first do their matrix products at once and
+  // the vector work (the softmax, the next tiles' way into LDS) after them, the
+  // second the other way round, so that one's matrix products meet the other's
+  // vector work (d = 256: 256 rows over 196,608 positions 1,790 -> 1,430 us; at d =
+  // 64, where the vector work is the most, all do the same).  (Two loops, as one loop with both orders spills; every wave
+  // passes j1 - j0 + 1 barriers in either.)
+  auto walk = [&](auto is_late) JF_INLINE {
+    constexpr bool late = decltype(is_late)::value;
+    Place at = {j0 * kTile / P, j0 * kTile % P};
+    int pid[4], slot[4];  // of tiles j - 1, j, j + 1, j + 2
+    pid[0] = -1, slot[0] = 0;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      pid[i] = page_of(at), slot[i] = at.slot;
+      step(at);
+    }
+    fetch_k(slot[1], pid[1]);
+    exps = exps_next;
+    deposit_k(j0);
+    fetch_v(slot[1], pid[1]);
+    fetch_k(slot[2], pid[2]);
+    for (int j = j0; j <= j1; ++j) {
+      __syncthreads();  // K of tile j and V of tile j - 1 are in LDS
+      const int pid_n = page_of(at);
+      uint32_t exps_1 = exps_next;
+      auto transport = [&]() JF_INLINE {
+        if (j < j1) {
+          deposit_v(j);
+          fetch_v(slot[2], pid[2]);
+        }
+        if (j + 1 < j1) {
+          deposit_k(j + 1);
+          fetch_k(slot[3], pid[3]);
+        }
+      };
+      if constexpr (late) {
+        if (active && j > j0) softmax(j - 1, (uint32_t)pid[0] < (uint32_t)num_pages);
+        transport();
+      }
+      __builtin_amdgcn_s_setprio(1);
+      if (active) {
+        if (j > j0) values(j - 1);
+        if (j < j1) scores(j);
+      }
+      __builtin_amdgcn_s_setprio(0);
+      if constexpr (!late) {
+        if (active && j < j1) softmax(j, (uint32_t)pid[1] < (uint32_t)num_pages);
+        transport();
+      }
+      exps = exps_1;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) pid[i] = pid[i + 1], slot[i] = slot[i + 1];
+      pid[3] = pid_n, slot[3] = at.slot;
+      step(at);
+    }
+  };
+  if (j0 < j1) {
+    if (D > 64 && wave >= kWaves / 2)
+      walk(std::true_type{});
+    else
+      walk(std::false_type{});
   }
 
   // ---- rows out, or partials
