@@ -81,7 +81,7 @@ jf_status check_chunk(const jf_kv_layout* L, int32_t T, int32_t num_q_heads, int
   if ((int64_t)prefix_len + T > INT32_MAX - 16384)
     return fail(JF_ERR_INVALID, "prefix_len + T overflows int32");
   if ((int64_t)T * num_q_heads > INT32_MAX || (int64_t)T * num_q_heads * (L->head_dim / 4) > kMaxThreads ||
-      ((int64_t)prefix_len + T + 255) * L->num_kv_heads > kMaxThreads)
+      ((int64_t)prefix_len + T + 255) * L->num_kv_heads * 2 > kMaxThreads)
     return fail(JF_ERR_UNSUPPORTED, "T * num_q_heads or the positions of all KV heads too large for one launch");
   return JF_OK;
 }

@@ -489,28 +489,41 @@ __global__ __launch_bounds__(256) void kv8_prefill_combine_kernel(
 //
 // A wave owns 16 NS positions, whose K it holds as matrix operands in
 // registers, and walks over all columns that see them; the columns' queries
-// (B operands) and (lse, row) pass through LDS, 64 columns at a time, shared
-// by the block's four waves.  No two waves add to the same position, so the
-// sums' order is fixed.  Weights are never rounded below fp32.
+// (B operands) and (lse, row) pass through LDS, shared by the block's four
+// waves.  No two waves add to the same position, so the sums' order is fixed.
+// Weights are never rounded below fp32.  Bound by the matrix cores (2 d flops per
+// score), and at d <= 128 as much by the vector work (an exponential, a fused
+// product and a sum per score); K is read once, Q once per 64 NS positions (from
+// the L2 of the head's XCD).
 constexpr int kWWaves = 4;
 constexpr int kWThreads = 64 * kWWaves;
-constexpr int kWCols = 64;
+
+// a + b columns, as (row, head) with head < gq
+struct Column {
+  int row, head;
+  __device__ __forceinline__ void advance(int rows, int heads, int gq) {
+    row += rows, head += heads;
+    if (head >= gq) head -= gq, ++row;
+  }
+};
 
 template <int D, bool BF16, int NS>
-__global__ __launch_bounds__(kWThreads) void kv8_weights_kernel(
+__global__ __launch_bounds__(kWThreads, NS > 2 ? 2 : 3) void kv8_weights_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
     const uint16_t* __restrict__ q, const float* __restrict__ lse,
     const int32_t* __restrict__ table, float* __restrict__ weights, int64_t stride, int Hq, int Hkv,
     int P, int block_shift, int num_pages, int T, int prefix, float scale_log2) {
-  constexpr int C = D / 64;
-  constexpr int kItems = kWCols * D * 2 / 16 / kWThreads;
-  __shared__ __align__(16) u32x4 qs[2][kWCols * D / 8];  // [16 columns][c][j][lane]
-  __shared__ float s_lse[2][kWCols];
-  __shared__ int s_row[2][kWCols];
+  constexpr int C = D / 64, kCols = D > 128 ? 32 : 64;  // columns in LDS at a time
+  constexpr int kItems = kCols * D * 2 / 16 / kWThreads;
+  constexpr int kEvery = C > 2 ? C / 2 : 1;              // items of a thread in one group of 16 columns
+  constexpr int kStep = C > 2 ? 16 : 16 * 2 / C;         // columns from one such run to the next
+  __shared__ __align__(16) u32x4 qs[2][kCols * D / 8];   // [16 columns][c][half][lane]
+  __shared__ float s_lse[2][kCols];
+  __shared__ int s_row[2][kCols];
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kv = blockIdx.x % Hkv, gq = Hq / Hkv;
-  const int64_t ncols = (int64_t)T * gq;
+  const int ncols = T * gq;
   const int L = prefix + T;
   const int64_t base = (int64_t)(blockIdx.x / Hkv) * (kWWaves * 16 * NS);
   const int64_t key0_64 = base + wave * 16 * NS;
@@ -536,79 +549,110 @@ __global__ __launch_bounds__(kWThreads) void kv8_weights_kernel(
   }
   float w[NS][4] = {};
 
-  // columns from the first row that sees the block's first key
-  const int64_t col0 = max((int64_t)0, base - prefix) * gq / kWCols * kWCols;
-  u32x4 stage[kItems];
-  float stage_lse = 0.0f;
-  int stage_row = 0;
-  auto fetch = [&](int64_t at) {
+  // columns from the first row that sees the block's first key; (row, head) of the
+  // columns that this thread brings to LDS are stepped without divisions
+  const int col0 = (int)(max((int64_t)0, base - prefix) * gq / kCols * kCols);
+  const int step_r = kStep / gq, step_h = kStep % gq, lse_r = kCols / gq, lse_h = kCols % gq;
+  Column qc, lc;
+  {
+    const int c = col0 + 16 * (wave / (2 * C)) + n, d = col0 + tid % kCols;
+    qc = {c / gq, c % gq}, lc = {d / gq, d % gq};
+  }
+  // what a thread brings to LDS for one turn; two turns are on their way
+  struct Stage {
+    u32x4 x[kItems];
+    float lse;
+    int row;
+  };
+  const uint16_t* const qh = q + (size_t)kv * gq * D + 16 * g;
+  auto fetch = [&](Stage& st) JF_INLINE {
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int i = tid + k * kWThreads;  // [16 columns][c][j][lane]
-      const int ln = i & 63, cj = (i >> 6) % (2 * C), grp = (i >> 6) / (2 * C);
-      const int64_t col = min(at + 16 * grp + (ln & 15), ncols - 1);
-      stage[k] = *reinterpret_cast<const u32x4*>(q + ((size_t)(col / gq) * Hq + kv * gq + col % gq) * D +
-                                                 64 * (cj >> 1) + 16 * (ln >> 4) + 8 * (cj & 1));
+      const int cj = (wave + kWWaves * k) % (2 * C);
+      st.x[k] = *reinterpret_cast<const u32x4*>(
+          qh + ((size_t)min(qc.row, T - 1) * Hq + qc.head) * D + 64 * (cj >> 1) + 8 * (cj & 1));
+      if ((k + 1) % kEvery == 0) qc.advance(step_r, step_h, gq);
     }
-    if (tid < kWCols) {
-      const int64_t col = at + tid, cc = min(col, ncols - 1);
-      stage_row = (int)(cc / gq);
-      const float z = lse[(size_t)stage_row * Hq + kv * gq + cc % gq];
-      // a row that sees nothing, and columns past the end, weigh nothing
-      stage_lse = col < ncols && z != -INFINITY ? z * kLog2e : INFINITY;
+    st.row = lc.row;
+    if (tid < kCols) {
+      st.lse = lse[(size_t)min(lc.row, T - 1) * Hq + kv * gq + lc.head];
+      lc.advance(lse_r, lse_h, gq);
     }
   };
-  if (col0 < ncols) {
-    fetch(col0);
-    int buf = 0;
-    for (int64_t at = col0; at < ncols; at += kWCols, buf ^= 1) {
+  auto turn = [&](Stage& st, int buf) JF_INLINE {
 #pragma unroll
-      for (int k = 0; k < kItems; ++k) qs[buf][tid + k * kWThreads] = stage[k];
-      if (tid < kWCols) s_lse[buf][tid] = stage_lse, s_row[buf][tid] = stage_row;
+      for (int k = 0; k < kItems; ++k) qs[buf][tid + k * kWThreads] = st.x[k];
+      if (tid < kCols) {
+        // a row that sees nothing, and columns past the end, weigh nothing
+        s_lse[buf][tid] = st.row < T && st.lse != -INFINITY ? st.lse * kLog2e : INFINITY;
+        s_row[buf][tid] = min(st.row, T - 1);
+      }
       __syncthreads();
-      if (at + kWCols < ncols) fetch(at + kWCols);
-      if (on) {
+      fetch(st);
+      if (!on) return;
+      // whether all columns of the stage see all of the wave's keys (rows ascend)
+      const bool whole = key0 + 16 * NS - 1 <= prefix + __builtin_amdgcn_readfirstlane(s_row[buf][0]);
 #pragma unroll
-        for (int grp = 0; grp < kWCols / 16; ++grp) {
-          f32x4 s[NS];
+      for (int grp = 0; grp < kCols / 16; grp += 2) {
+        f32x4 s[2][NS];
 #pragma unroll
-          for (int t = 0; t < NS; ++t) s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int c = 0; c < C; ++c)
+          for (int t = 0; t < NS; ++t) s[u][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const u32x4 b = qs[buf][((grp * C + c) * 2 + j) * 64 + lane];
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-              for (int t = 0; t < NS; ++t) s[t] = mma<BF16>(kf[t][c][j], b, s[t]);
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const u32x4 b = qs[buf][(((grp + u) * C + c) * 2 + j) * 64 + lane];
+#pragma unroll
+              for (int t = 0; t < NS; ++t) s[u][t] = mma<BF16>(kf[t][c][j], b, s[u][t]);
             }
-          const float z = s_lse[buf][16 * grp + n];
-          const int see = prefix + s_row[buf][16 * grp + n];  // the last position it sees
-          if (__any(key0 + 16 * NS - 1 > see)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float z = s_lse[buf][16 * (grp + u) + n];
+          if (!whole) {
+            const int see = prefix + s_row[buf][16 * (grp + u) + n];  // the last position the column sees
 #pragma unroll
             for (int t = 0; t < NS; ++t)
 #pragma unroll
               for (int i = 0; i < 4; ++i)
-                w[t][i] += key0 + 16 * t + 4 * g + i > see ? 0.0f : exp2_(fmaf(s[t][i], f[t], -z));
+                w[t][i] += key0 + 16 * t + 4 * g + i > see ? 0.0f : exp2_(fmaf(s[u][t][i], f[t], -z));
           } else {
 #pragma unroll
             for (int t = 0; t < NS; ++t)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) w[t][i] += exp2_(fmaf(s[t][i], f[t], -z));
+              for (int i = 0; i < 4; ++i) w[t][i] += exp2_(fmaf(s[u][t][i], f[t], -z));
           }
         }
       }
+  };
+  if (col0 < ncols) {
+    Stage s0, s1;
+    fetch(s0);
+    fetch(s1);
+    for (int at = col0; at < ncols; at += 2 * kCols) {
+      turn(s0, 0);
+      if (at + kCols < ncols) turn(s1, 1);
     }
   }
   if (!on) return;
+  // Sums over the 16 lanes that share the positions: halved turn by turn, until
+  // lane n holds the sum of position 16 (n / 4) + 4 g + n % 4.
+  float v[4 * NS];
 #pragma unroll
-  for (int t = 0; t < NS; ++t)
+  for (int i = 0; i < 4 * NS; ++i) v[i] = w[i / 4][i % 4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+  for (int o = 2 * NS; o; o >>= 1)
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) w[t][i] += __shfl_xor(w[t][i], o);
-      const int pos = key0 + 16 * t + 4 * g + i;
-      if (n == 4 * t % 16 + i && pos < L) weights[(size_t)kv * stride + pos] += w[t][i];
+    for (int k = 0; k < o; ++k) {
+      const bool up = (n & o) != 0;
+      v[k] = (up ? v[k + o] : v[k]) + __shfl_xor(up ? v[k] : v[k + o], o);
     }
+  if (NS == 2) v[0] += __shfl_xor(v[0], 8);
+  const int pos = key0 + 16 * (n / 4) + 4 * g + n % 4;
+  if (n < 4 * NS && pos < L) weights[(size_t)kv * stride + pos] += v[0];
 }
 
 template <int D, bool BF16>
@@ -706,9 +750,23 @@ hipError_t launch_kv8_weights(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool
   auto go = [&](auto fn) {
     return fn(L, pool, q, lse, T, Hq, block_table, prefix_len, softmax_scale, weights, stride, stream);
   };
-  if (L.head_dim == 64) return bf16 ? go(launch_weights_t<64, true, 4>) : go(launch_weights_t<64, false, 4>);
-  if (L.head_dim == 128) return bf16 ? go(launch_weights_t<128, true, 4>) : go(launch_weights_t<128, false, 4>);
-  return bf16 ? go(launch_weights_t<256, true, 4>) : go(launch_weights_t<256, false, 4>);
+  // Few columns over many positions: 64 positions per wave, for fewer starts; else
+  // 32, for an even chip.  64 rows, 32/8 heads of 128, 65,472 positions 57 us
+  // against 72, 24/4 heads of 256, 30,000 34 against 44; but 8,000 positions 14.3
+  // against 12.7, and 2,048 rows without a prefix 188 against 134.
+  const int64_t keys = (int64_t)prefix_len + T;
+  const bool four = (int64_t)T * (Hq / L.num_kv_heads) <= 1024 &&
+                    keys / 256 * L.num_kv_heads >= num_cus() * 3 / 2;
+#define JF_CASE(D_)                                                                          \
+  if (L.head_dim == D_) {                                                                    \
+    if (four) return bf16 ? go(launch_weights_t<D_, true, 4>) : go(launch_weights_t<D_, false, 4>); \
+    return bf16 ? go(launch_weights_t<D_, true, 2>) : go(launch_weights_t<D_, false, 2>);    \
+  }
+  JF_CASE(64)
+  JF_CASE(128)
+  JF_CASE(256)
+#undef JF_CASE
+  return hipErrorInvalidValue;
 }
 
 }  // namespace jfkv

@@ -265,6 +265,8 @@ CHUNKS = [
     (64, 3, 3, 64, 64, True, 300, 3),
     (256, 1, 2, 128, 32, False, 3, 2500),
     (64, 2, 24, 128, 16, False, 40, 200),
+    (256, 8, 8, 64, 64, True, 5, 13000),   # few columns over many positions
+    (256, 8, 8, 128, 128, False, 6, 12500),
 ]
 
 
