@@ -305,23 +305,58 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
   uint8_t* const exps = is_v ? v_exps : k_exps;
   uint8_t* const to = codes + (run * P + j0 % P) * D;
 
-  for (int t = tid; t < block; t += nthr) {
-    int src = -1, slot = 0, e = -126;
-    if (t < live) {
-      const int pos = kept[((size_t)b * Hkv + h) * keep + j0 + t];
+  if (tid < block) {  // (there are at least four threads per token)
+    int src = -1, slot = 0;
+    if (tid < live) {
+      const int pos = kept[((size_t)b * Hkv + h) * keep + j0 + tid];
       const int pg = src_tables[(size_t)b * max_pages + pos / P];
       slot = pos % P;
-      if ((uint32_t)pg < (uint32_t)num_pages) {
-        src = pg * Hkv + h;
-        e = (int)exps[(size_t)src * (P / block) + slot / block] - 127;
-      }
+      if ((uint32_t)pg < (uint32_t)num_pages) src = pg * Hkv + h;
     }
-    s_run[t] = src, s_slot[t] = slot, s_exp[t] = e;
+    s_run[tid] = src, s_slot[tid] = slot;
   }
   __syncthreads();
+  // The exponents are on their way along with the codes.
+  int e = -126;
+  if (tid < block && s_run[tid] >= 0)
+    e = (int)exps[(size_t)s_run[tid] * (P / block) + (s_slot[tid] >> __builtin_ctz(block))] - 127;
 
+  // A token without a page reads the pool's first one and counts as zeros: no
+  // branch stands between the loads.
+  const int dl = __builtin_ctz(D);
   uint32_t raw[NI][4];  // K: 16 dims of a token; V: four dims of four tokens
-  int top = -126;       // the least exponent that the values seen allow
+#pragma unroll
+  for (int k = 0; k < NI; ++k) {
+    const int i = tid + k * nthr;
+    if (!is_v) {
+      const int t = i >> (dl - 4), c = i & (D / 16 - 1), run = s_run[t];
+      const uint4 a = *reinterpret_cast<const uint4*>(
+          codes + ((size_t)max(run, 0) * P + s_slot[t]) * D + 16 * c);
+      raw[k][0] = run < 0 ? 0u : a.x, raw[k][1] = run < 0 ? 0u : a.y;
+      raw[k][2] = run < 0 ? 0u : a.z, raw[k][3] = run < 0 ? 0u : a.w;
+    } else {
+      const int r = i & (D - 1), t0 = (i >> dl) * 16 + (r % 64) / 16 * 4;
+      uint4 a[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int slot = s_slot[t0 + j];
+        a[j] = *reinterpret_cast<const uint4*>(
+            codes + ((size_t)max(s_run[t0 + j], 0) * P + slot / 16 * 16) * D + r / 64 * 1024 +
+            slot % 16 / 4 * 256 + r % 16 * 16);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int s = 8 * (s_slot[t0 + j] % 4);
+        const uint32_t m = s_run[t0 + j] < 0 ? 0u : 255u;
+        raw[k][j] = ((a[j].x >> s) & m) | ((a[j].y >> s) & m) << 8 | ((a[j].z >> s) & m) << 16 |
+                    ((a[j].w >> s) & m) << 24;
+      }
+    }
+  }
+  if (tid < block) s_exp[tid] = e;
+  __syncthreads();
+
+  int top = -126;  // the least exponent that the values allow
   auto look = [&](uint32_t w, int e) {
     const uint32_t a = max(max(w & 0x7fu, (w >> 8) & 0x7fu), max((w >> 16) & 0x7fu, (w >> 24) & 0x7fu));
     if (a && a != 0x7fu) top = max(top, e + exponent_for(__builtin_amdgcn_cvt_f32_fp8((int)a, 0)));
@@ -329,32 +364,9 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
 #pragma unroll
   for (int k = 0; k < NI; ++k) {
     const int i = tid + k * nthr;
+    const int t0 = is_v ? (i >> dl) * 16 + (i % 64) / 16 * 4 : i >> (dl - 4);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) raw[k][j] = 0u;
-    if (!is_v) {
-      const int t = i / (D / 16), c = i % (D / 16);
-      if (s_run[t] >= 0) {
-        const uint4 a = *reinterpret_cast<const uint4*>(codes + ((size_t)s_run[t] * P + s_slot[t]) * D + 16 * c);
-        raw[k][0] = a.x, raw[k][1] = a.y, raw[k][2] = a.z, raw[k][3] = a.w;
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) look(raw[k][j], s_exp[t]);
-    } else {
-      const int r = i % D, t0 = (i / D) * 16 + (r % 64) / 16 * 4;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int t = t0 + j;
-        if (s_run[t] < 0) continue;
-        const int slot = s_slot[t];
-        const uint4 a = *reinterpret_cast<const uint4*>(
-            codes + ((size_t)s_run[t] * P + slot / 16 * 16) * D + r / 64 * 1024 +
-            slot % 16 / 4 * 256 + r % 16 * 16);
-        const int s = 8 * (slot % 4);
-        raw[k][j] = ((a.x >> s) & 255u) | ((a.y >> s) & 255u) << 8 | ((a.z >> s) & 255u) << 16 |
-                    ((a.w >> s) & 255u) << 24;
-        look(raw[k][j], s_exp[t]);
-      }
-    }
+    for (int j = 0; j < 4; ++j) look(raw[k][j], s_exp[is_v ? t0 + j : t0]);
   }
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = max(top, __shfl_xor(top, o));
@@ -367,13 +379,13 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
     const int i = tid + k * nthr;
     uint4* const dst = reinterpret_cast<uint4*>(to) + i;
     if (!is_v) {
-      const int t = i / (D / 16);
+      const int t = i >> (dl - 4);
       if (t >= live) continue;
       const float f = __builtin_ldexpf(1.0f, s_exp[t] - top);
       *dst = make_uint4(rescale4(raw[k][0], f), rescale4(raw[k][1], f), rescale4(raw[k][2], f),
                         rescale4(raw[k][3], f));
     } else {
-      const int r = i % D, t0 = (i / D) * 16 + (r % 64) / 16 * 4;
+      const int t0 = (i >> dl) * 16 + (i % 64) / 16 * 4;
       if (t0 >= live) continue;
       uint32_t c[4], o[4];
 #pragma unroll
