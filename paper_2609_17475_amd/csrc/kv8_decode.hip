@@ -1,13 +1,14 @@
 // Decode attention over the 8-bit cache (format: jfkv_kv8.h): 1-4 causal query
-// tokens per request, split over the positions, with an in-kernel combine, and
-// optionally the attention weights of the call added up per position.
+// tokens per request, split over the positions, whose partial results are joined
+// by the last block to finish or a second launch, and optionally the attention
+// weights of the call added up per position by another.
 //
 //   s_t = scale * q . k_t,  p_t = exp(s_t - max s),  o = sum p_t v_t / sum p_t
 //
 // One pass over the pages with a running maximum m and sum l per query (online
 // softmax).  The (token, head) pairs that read one KV head are the 16 columns
-// of the matrix products (more pairs: further blocks on the same XCD, which
-// find the pages in its L2):
+// of the matrix products (up to 32 pairs: two sets of them for each widened code;
+// more: further blocks on the same XCD, which find the pages in its L2):
 //   scores  A = K (16 positions x 32 dims), B = Q: lane (n, g) receives column
 //           n at positions 4 g .. 4 g + 3;
 //   values  A = V (16 dims x 32 positions), B = P: the lane's own eight scores
@@ -21,7 +22,10 @@
 // P stays below 2^14 in fp16.  Scores, m, l and the accumulators are fp32; P is
 // rounded to fp16 (2^-11 relative, averaged over the positions).
 //
-// HBM-bound: 2 (d + 1 / block) bytes per position and KV head.
+// HBM-bound where it is long: 2 (d + 1 / block) bytes per position and KV head.
+// One request of 262,144 positions, 32/8 heads of 128, takes 84 us, 6.4 TB/s; of
+// 4,097, 4/1 heads, 8.5 us: a launch, three loads that wait for one another, and
+// the join.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -39,10 +43,22 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRow = 32;       // positions a wave takes at a time (in one page)
 constexpr int kCols = 16;      // (token, head) pairs of a block
 constexpr int kXcds = 8;
-constexpr int kGroups = 16;    // groups of splits that are joined first, at most
 constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
 constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
 constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
+
+// Splits of a request of L positions.  Rows per wave below which it is not cut
+// further: every split costs a start, a merge and a record.  24/4 heads, d = 256,
+// 4 / 5 / 6 rows: 4 x 20,000 positions 40 / 36 / 38 us (three tokens 46 / 40 /
+// 42), 16 x 4,097 46 / 37 / 39, one request of 4,097 13.9 / 15.3 / 16.5.  32/8
+// heads, d = 128, 2 / 3 / 4 rows: 32 x 4,097 72 / 66 / 72, 8 x 9,000 37 / 36 / 37,
+// one of 4,097 9.2 / 10.1 / 10.8.
+template <int D, int CS>
+__device__ __forceinline__ int splits_of(int L, int split_cap) {
+  constexpr int kMinRows = D > 128 ? 5 : 3;
+  const int rows = (L + kRow - 1) / kRow;
+  return max(1, min(split_cap, (rows + kWaves * kMinRows - 1) / (kWaves * kMinRows)));
+}
 
 template <int D>
 struct Row {
@@ -65,15 +81,65 @@ __device__ __forceinline__ float col_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// Partial results of some splits: sums of p v and p in units of 2^m.
+struct Joined {
+  f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, den = 0.0f;
+  __device__ __forceinline__ f32x4 out() const { return num * (den > 0.0f ? 1.0f / den : 0.0f); }
+  __device__ __forceinline__ float lse() const { return den > 0.0f ? m + log2f(den) : INFINITY; }
+};
+
+// A request's records are joined in one order whichever kernel does it: parts of
+// kAt splits by any threads (their loads are in flight together), then the parts
+// from the first to the last.
+constexpr int kAt = 8;
+struct Parts {
+  f32x4* num;
+  f32x2* ml;
+  // the sums of the first `count` of eight records, as part u
+  __device__ __forceinline__ void put(int u, const f32x4 (&o)[kAt], const f32x2 (&r)[kAt],
+                                      int count) const {
+    float m = r[0].x;
+#pragma unroll
+    for (int k = 1; k < kAt; ++k) m = fmaxf(m, r[k].x);  // (behind count: repeated ones)
+    f32x4 n = {0.0f, 0.0f, 0.0f, 0.0f};
+    float den = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) {
+      const float f = k >= count || r[k].x == -INFINITY ? 0.0f : exp2_(r[k].x - m);
+      n += o[k] * f;
+      den = fmaf(f, r[k].y, den);
+    }
+    num[u] = n, ml[u] = f32x2{m, den};
+  }
+  // item i of `items` over all parts
+  __device__ __forceinline__ Joined get(int i, int items, int parts) const {
+    Joined a;
+    for (int u = 0; u < parts; ++u) a.m = fmaxf(a.m, ml[u * items + i].x);
+    for (int u = 0; u < parts; ++u) {
+      const f32x2 r = ml[u * items + i];
+      const float f = r.x == -INFINITY ? 0.0f : exp2_(r.x - a.m);
+      a.num += num[u * items + i] * f;
+      a.den = fmaf(f, r.y, a.den);
+    }
+    return a;
+  }
+};
+__device__ __forceinline__ Parts parts_at(float* smem, int count) {
+  f32x4* const num = reinterpret_cast<f32x4*>(smem);
+  return {num, reinterpret_cast<f32x2*>(num + count)};
+}
+constexpr size_t kPartBytes = sizeof(f32x4) + sizeof(f32x2);
+
 template <int D, bool BF16, bool SUMS, int CS>
-__global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 1 : 3) void kv8_decode_kernel(
+__global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 2 : 3) void kv8_decode_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
     const uint16_t* __restrict__ q, const int32_t* __restrict__ block_tables,
     const int32_t* __restrict__ seq_lens, uint32_t* __restrict__ tickets, float* __restrict__ recs,
     float* __restrict__ lse, float* __restrict__ logits, uint16_t* __restrict__ out, int Hq, int sq,
     int Hkv, int P, int block_shift, int num_pages, int max_pages, int max_splits, int split_cap,
-    int n_hchunks, int group_splits, float scale_log2) {
+    int n_hchunks, bool apart, float scale_log2) {
   constexpr int C = D / 64;
   constexpr int kPart = D + 4;  // floats of a partial: o, m, l (16-byte rows)
   extern __shared__ __align__(16) float smem[];
@@ -91,21 +157,19 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 1 : 3) void kv8_decod
   const int c0 = hc * kCols * CS, ncols = min(kCols * CS, pairs - c0);
 
   const int L = min(max(seq_lens[b], 0), max_pages * P);
-  const int rows = (L + kRow - 1) / kRow;
-  // Rows per wave below which a request is not cut further: every split costs a
-  // start, a merge and a record.  24/4 heads, d = 256, 2 / 3 / 4 rows: 4 x 20,000
-  // positions 48 / 46 / 43 us (3 query tokens 76 / 67 / 61), 4,097 13.6 / 15.2 /
-  // 16.5; 32/8 heads, d = 128: 8 x 9,000 41 / 38 / 39, 4,097 9.6 / 9.4 / 10.0.
-  constexpr int kMinRows = D > 128 && CS > 1 ? 4 : 3;
-  const int S = max(1, min(split_cap, (rows + kWaves * kMinRows - 1) / (kWaves * kMinRows)));
+  const int rows = (L + kRow - 1) / kRow, S = splits_of<D, CS>(L, split_cap);
   if (split >= S) return;
   const int base = rows / S, rem = rows % S;
   const int r0 = split * base + min(split, rem), r1 = r0 + base + (split < rem ? 1 : 0);
 
   // ---- the block's queries as B operands: column n of each set, dims 64 c +
-  // 16 g + 8 j ..
+  // 16 g + 8 j ..  In registers, or in LDS where two sets of d = 256 would leave
+  // room for one block per CU only (three query tokens of 24/4 heads, 4 x 20,000
+  // positions: 61 -> 56 us when that was done).
+  constexpr bool kQLds = D > 128 && CS > 1;
   int see[CS];  // positions the columns' queries see
   u32x4 qf[CS][C][2];
+  u32x4* const s_q = reinterpret_cast<u32x4*>(smem);
 #pragma unroll
   for (int cs = 0; cs < CS; ++cs) {
     const int pair = c0 + min(kCols * cs + n, ncols - 1);  // (columns without a pair repeat the last one)
@@ -116,8 +180,15 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 1 : 3) void kv8_decod
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        qf[cs][c][j] = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j);
+        if (!kQLds || wave == c % kWaves) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j);
+          if (kQLds)
+            s_q[64 * ((cs * C + c) * 2 + j) + lane] = x;
+          else
+            qf[cs][c][j] = x;
+        }
   }
+  if (kQLds) __syncthreads();
 
   f32x4 acc[CS][C][4] = {};
   float m[CS], l[CS];
@@ -175,24 +246,32 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 1 : 3) void kv8_decod
   // scores of a row in log2 units, and the exponents of its values
   auto scores = [&](const Row<D>& w, int r, float (&s)[CS][2][4], int (&ev)[2]) {
     const int pos0 = r * kRow;
+    f32x4 a[2][CS] = {};
+    int ql = lane;
+    asm volatile("" : "+v"(ql));  // (opaque: LDS is not read ahead of the page walk)
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        u32x4 qc[CS];
+#pragma unroll
+        for (int cs = 0; cs < CS; ++cs)
+          qc[cs] = kQLds ? s_q[64 * ((cs * C + c) * 2 + j) + ql] : qf[cs][c][j];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 k = widen8<BF16>(w.k[t][c][2 * j], w.k[t][c][2 * j + 1]);
+#pragma unroll
+          for (int cs = 0; cs < CS; ++cs) a[t][cs] = mma<BF16>(k, qc[cs], a[t][cs]);
+        }
+      }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      f32x4 a[CS] = {};
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const u32x4 k0 = widen8<BF16>(w.k[t][c].x, w.k[t][c].y);
-        const u32x4 k1 = widen8<BF16>(w.k[t][c].z, w.k[t][c].w);
-#pragma unroll
-        for (int cs = 0; cs < CS; ++cs) a[cs] = mma<BF16>(k0, qf[cs][c][0], a[cs]);
-#pragma unroll
-        for (int cs = 0; cs < CS; ++cs) a[cs] = mma<BF16>(k1, qf[cs][c][1], a[cs]);
-      }
       const float f = scale_log2 * power2(lane_value(w.exps, t) - 127);
       ev[t] = lane_value(w.exps, 2 + t) - 127;
 #pragma unroll
       for (int cs = 0; cs < CS; ++cs)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[cs][t][i] = a[cs][i] * f;
+        for (int i = 0; i < 4; ++i) s[cs][t][i] = a[t][cs][i] * f;
     }
     if (pos0 + kRow > L - sq + 1) {
       // positions that a query does not see, and slots not written yet (their codes,
@@ -337,163 +416,145 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 1 : 3) void kv8_decod
     }
   }
 
-  // ---- merge the waves in LDS: o (units 1), m, l of the block's columns
-#pragma unroll
-  for (int cs = 0; cs < CS; ++cs) {
-    const float den = col_sum(l[cs]);
-    const int col = kCols * cs + n;
-    float* part = smem + (size_t)(wave * ncols + col) * kPart;
-    if (col < ncols) {
-      const float f = __builtin_ldexpf(1.0f, e_ref);
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4*>(part + 64 * c + 16 * g + 4 * i) =
-              f32x4{acc[cs][c][0][i], acc[cs][c][1][i], acc[cs][c][2][i], acc[cs][c][3][i]} * f;
-      if (g == 0) part[D] = m[cs], part[D + 1] = den;
-    }
-  }
-  __syncthreads();
   const size_t rec0 = ((size_t)b * Hkv + kv) * pairs + c0;  // the block's first (request, pair)
   // the block's records, written and read with device-scope coherent accesses
   const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
       recs + rec0 * max_splits * kPart, (short)0, (int)(ncols * max_splits * kPart * 4), 0x00020000);
   constexpr int kSc1 = 16;
-  auto store_rec = [&](int col, int at, int d4, int ml0, f32x4 o, float M, float den) {
-    const int rec = (col * max_splits + at) * kPart * 4;
+  auto store_rec = [&](int col, int d4, f32x4 o, float M, float den) {
+    const int rec = (col * max_splits + split) * kPart * 4;
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rs, rec + 16 * d4, 0, kSc1);
     if (d4 == 0)
       __builtin_amdgcn_raw_buffer_store_b64(
-          __builtin_bit_cast(u32x2, f32x2{M, den}), rs, rec + 4 * (D + ml0), 0, kSc1);
+          __builtin_bit_cast(u32x2, f32x2{M, den}), rs, rec + 4 * D, 0, kSc1);
   };
   auto store_out = [&](int col, int d4, f32x4 o) {
     const int pr = c0 + col;
     uint16_t* op = out + (((size_t)b * sq + pr / gq) * Hq + kv * gq + pr % gq) * D + 4 * d4;
     *reinterpret_cast<uint2*>(op) = make_uint2(narrow2<BF16>(o.x, o.y), narrow2<BF16>(o.z, o.w));
   };
-  for (int i = tid; i < ncols * (D / 4); i += kThreads) {
-    const int col = i / (D / 4), d4 = i % (D / 4);
-    float mw[kWaves], M = -INFINITY, den = 0.0f;
+  // ---- merge the waves in LDS, one set of columns after the other: o (units 1),
+  // m, l
+  const int wide = min(kCols, ncols) * kPart;  // floats of a wave
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      mw[w] = smem[(size_t)(w * ncols + col) * kPart + D];
-      M = fmaxf(M, mw[w]);
-    }
-    f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int cs = 0; cs < CS; ++cs) {
+    const int here = min(kCols, ncols - kCols * cs);  // columns of the set
+    const float den = col_sum(l[cs]);
+    float* const mine = smem + wave * wide + n * kPart;
+    if (kQLds || cs) __syncthreads();  // (LDS still held the queries or the last set)
+    if (n < here) {
+      const float f = __builtin_ldexpf(1.0f, e_ref);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float* part = smem + (size_t)(w * ncols + col) * kPart;
-      const float f = mw[w] == -INFINITY ? 0.0f : exp2_(mw[w] - M);
-      num += *reinterpret_cast<const f32x4*>(part + 4 * d4) * f;
-      den = fmaf(f, part[D + 1], den);
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4*>(mine + 64 * c + 16 * g + 4 * i) =
+              f32x4{acc[cs][c][0][i], acc[cs][c][1][i], acc[cs][c][2][i], acc[cs][c][3][i]} * f;
+      if (g == 0) mine[D] = m[cs], mine[D + 1] = den;
     }
-    if (S == 1) {
-      store_out(col, d4, num * (den > 0.0f ? 1.0f / den : 0.0f));
-      if (SUMS && d4 == 0) lse[rec0 + col] = den > 0.0f ? M + log2f(den) : INFINITY;
-    } else {
-      store_rec(col, split, d4, 0, num, M, den);
+    __syncthreads();
+    for (int i = tid; i < here * (D / 4); i += kThreads) {
+      const int at = i / (D / 4), col = kCols * cs + at, d4 = i % (D / 4);
+      const float* const part = smem + at * kPart;
+      float mw[kWaves], M = -INFINITY, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        mw[w] = part[w * wide + D];
+        M = fmaxf(M, mw[w]);
+      }
+      f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = mw[w] == -INFINITY ? 0.0f : exp2_(mw[w] - M);
+        num += *reinterpret_cast<const f32x4*>(part + w * wide + 4 * d4) * f;
+        sum = fmaf(f, part[w * wide + D + 1], sum);
+      }
+      if (S == 1) {
+        store_out(col, d4, num * (sum > 0.0f ? 1.0f / sum : 0.0f));
+        if (SUMS && d4 == 0) lse[rec0 + col] = sum > 0.0f ? M + log2f(sum) : INFINITY;
+      } else {
+        store_rec(col, d4, num, M, sum);
+      }
     }
   }
-  if (S == 1) return;
+  if (S == 1 || apart) return;
 
-  // ---- the last split to finish combines the records; where they are many, the
-  // last of each group of splits first joins the group's (into its first record,
-  // m and l behind the split's own).  Every word the blocks exchange is written
+  // ---- the last split to finish combines the records.  Every word the blocks exchange is written
   // and read by device-scope coherent accesses (sc1: written through to, and read
   // from, the level that all XCDs share); each thread waits for its
   // record stores before the barrier that precedes the ticket, and the combining
   // block loads records only after it has seen the last ticket (the decode over
   // 4-bit pages argues this exchange in full).
   uint32_t* const s_ticket = reinterpret_cast<uint32_t*>(smem);
-  auto last_of = [&](uint32_t* ticket, int count) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-      const uint32_t t = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      if (t == (uint32_t)(count - 1))
-        __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      *s_ticket = t;
-    }
-    __syncthreads();
-    return *s_ticket == (uint32_t)(count - 1);
-  };
-  // Joins `count` records from `first` on, `step` apart, whose m and l lie at
-  // float D + ml; done(col, d4, num, den, M) gets the sums of four dims.  GR
-  // groups of threads share the records, kAt in flight each, and meet in LDS.
-  const int items = ncols * (D / 4), GR = min(max(kThreads / items, 1), 8);
-  f32x4* const s_num = reinterpret_cast<f32x4*>(smem) + 1;
-  float* const s_ml = reinterpret_cast<float*>(s_num + kThreads);
-  auto join = [&](int first, int count, int step, int ml0, auto&& done) {
-    constexpr int kAt = 8;
-    for (int i0 = 0; i0 < items; i0 += kThreads) {  // (one turn where GR > 1)
-      const int i = GR > 1 ? tid % items : i0 + tid, gr = GR > 1 ? tid / items : 0;
-      const bool on = i < items && gr < GR;
-      const int col = min(i, items - 1) / (D / 4), d4 = i % (D / 4);
-      float M = -INFINITY, den = 0.0f;
-      f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (on)
-        for (int s0 = gr; s0 < count; s0 += GR * kAt) {
-          f32x4 o[kAt];
-          f32x2 ml[kAt];
-#pragma unroll
-          for (int k = 0; k < kAt; ++k) {
-            const int at = (col * max_splits + first + min(s0 + k * GR, count - 1) * step) * kPart * 4;
-            o[k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at + 16 * d4, 0, kSc1));
-            ml[k] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, at + 4 * (D + ml0), 0, kSc1));
-          }
-          float mx = M;
-#pragma unroll
-          for (int k = 0; k < kAt; ++k) {
-            if (s0 + k * GR >= count) ml[k].x = -INFINITY;
-            mx = fmaxf(mx, ml[k].x);
-          }
-          const float f = M == -INFINITY ? 0.0f : exp2_(M - mx);
-          num *= f, den *= f, M = mx;
-#pragma unroll
-          for (int k = 0; k < kAt; ++k) {
-            const float fk = ml[k].x == -INFINITY ? 0.0f : exp2_(ml[k].x - M);
-            num += o[k] * fk;
-            den = fmaf(fk, ml[k].y, den);
-          }
-        }
-      if (GR > 1) {
-        s_num[tid] = num, s_ml[2 * tid] = M, s_ml[2 * tid + 1] = den;
-        __syncthreads();
-        if (gr == 0) {
-          for (int k = 1; k < GR; ++k) {
-            const int o = tid + k * items;
-            const float mo = s_ml[2 * o], mx = fmaxf(M, mo);
-            const float fa = M == -INFINITY ? 0.0f : exp2_(M - mx);
-            const float fb = mo == -INFINITY ? 0.0f : exp2_(mo - mx);
-            num = num * fa + s_num[o] * fb;
-            den = den * fa + s_ml[2 * o + 1] * fb;
-            M = mx;
-          }
-        }
-      }
-      if (on && gr == 0) done(col, d4, num, den, M);
-      if (GR > 1) break;
-    }
-  };
-  auto finish = [&](int col, int d4, f32x4 num, float den, float M) {
-    store_out(col, d4, num * (den > 0.0f ? 1.0f / den : 0.0f));
-    if (SUMS && d4 == 0) lse[rec0 + col] = den > 0.0f ? M + log2f(den) : INFINITY;
-  };
-  const size_t unit = ((size_t)b * Hkv + kv) * n_hchunks + hc;
-  // (a split that exceeds max_splits / group_splits groups does not exist)
-  const int GS = group_splits;
-  if (GS == 0 || S <= GS) {
-    if (last_of(tickets + unit * (GS ? kGroups + 1 : 1), S)) join(0, S, 1, 0, finish);
-    return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t* const ticket = tickets + ((size_t)b * Hkv + kv) * n_hchunks + hc;
+    const uint32_t t = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (t == (uint32_t)(S - 1))
+      __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *s_ticket = t;
   }
-  const int grp = split / GS, groups = (S + GS - 1) / GS;
-  uint32_t* const mine = tickets + unit * (kGroups + 1);
-  if (!last_of(mine + 1 + grp, min(GS, S - grp * GS))) return;
-  join(grp * GS, min(GS, S - grp * GS), 1, 0, [&](int col, int d4, f32x4 num, float den, float M) {
-    store_rec(col, grp * GS, d4, 2, num, M, den);
-  });
-  if (last_of(mine, groups)) join(0, groups, GS, 2, finish);
+  __syncthreads();
+  if (*s_ticket != (uint32_t)(S - 1)) return;
+  const int items = ncols * (D / 4), parts = (S + kAt - 1) / kAt;
+  const Parts at = parts_at(smem + 4, items * parts);
+  for (int u = tid; u < items * parts; u += kThreads) {
+    const int i = u % items, col = i / (D / 4), s0 = u / items * kAt;
+    f32x4 o[kAt];
+    f32x2 ml[kAt];
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) {
+      const int rec = (col * max_splits + min(s0 + k, S - 1)) * kPart * 4;
+      o[k] = __builtin_bit_cast(
+          f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, rec + 16 * (i % (D / 4)), 0, kSc1));
+      ml[k] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, rec + 4 * D, 0, kSc1));
+    }
+    at.put(u, o, ml, S - s0);
+  }
+  __syncthreads();
+  for (int i = tid; i < items; i += kThreads) {
+    const Joined sum = at.get(i, items, parts);
+    store_out(i / (D / 4), i % (D / 4), sum.out());
+    if (SUMS && i % (D / 4) == 0) lse[rec0 + i / (D / 4)] = sum.lse();
+  }
+}
+
+// The same where a launch of its own joins the records: a workgroup per (request,
+// KV head, pair).
+template <int D, bool BF16, bool SUMS, int CS>
+__global__ __launch_bounds__(kThreads) void kv8_join_kernel(
+    const float* __restrict__ recs, const int32_t* __restrict__ seq_lens, float* __restrict__ lse,
+    uint16_t* __restrict__ out, int Hq, int sq, int cap, int max_splits, int split_cap) {
+  constexpr int kPer = D / 4;
+  extern __shared__ __align__(16) float smem[];
+  const int pair = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, pairs = gridDim.x, Hkv = gridDim.y;
+  const int S = splits_of<D, CS>(min(max(seq_lens[b], 0), cap), split_cap);
+  if (S == 1) return;  // (the output is there)
+  const int tid = threadIdx.x, parts = (S + kAt - 1) / kAt;
+  const size_t rec = ((size_t)b * Hkv + kv) * pairs + pair;
+  const float* const from = recs + rec * max_splits * (D + 4);
+  const Parts at = parts_at(smem, kPer * parts);
+  for (int u = tid; u < kPer * parts; u += kThreads) {
+    const int s0 = u / kPer * kAt;
+    f32x4 o[kAt];
+    f32x2 ml[kAt];
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) {
+      const float* p = from + (size_t)min(s0 + k, S - 1) * (D + 4);
+      o[k] = *reinterpret_cast<const f32x4*>(p + 4 * (u % kPer));
+      ml[k] = *reinterpret_cast<const f32x2*>(p + D);
+    }
+    at.put(u, o, ml, S - s0);
+  }
+  __syncthreads();
+  if (tid >= kPer) return;
+  const int gq = Hq / Hkv;
+  const Joined sum = at.get(tid, kPer, parts);
+  const f32x4 r = sum.out();
+  uint16_t* op = out + (((size_t)b * sq + pair / gq) * Hq + kv * gq + pair % gq) * D + 4 * tid;
+  *reinterpret_cast<uint2*>(op) = make_uint2(narrow2<BF16>(r.x, r.y), narrow2<BF16>(r.z, r.w));
+  if (SUMS && tid == 0) lse[rec] = sum.lse();
 }
 
 // weights[b][kv][t] += sum over the pairs of exp2(s_t - lse): the decode left
@@ -511,11 +572,20 @@ __global__ __launch_bounds__(256) void kv8_sums_kernel(const float* __restrict__
   const size_t row = (size_t)b * Hkv + kv;
   const float* lg = logits + row * pairs * (size_t)cap + t;
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < pairs; ++i) {
-    const f32x4 s = *reinterpret_cast<const f32x4*>(lg + (size_t)i * cap);
-    const float z = lse[row * pairs + i];
+  constexpr int kAt = 6;  // loads on the way (one at a time: 9.1 us of 4 x 20,000 positions, 18 pairs)
+  for (int i0 = 0; i0 < pairs; i0 += kAt) {
+    f32x4 s[kAt];
+    float z[kAt];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += exp2_(s[e] - z);
+    for (int k = 0; k < kAt; ++k) {
+      const int i = min(i0 + k, pairs - 1);
+      s[k] = *reinterpret_cast<const f32x4*>(lg + (size_t)i * cap);
+      z[k] = i0 + k < pairs ? lse[row * pairs + i] : INFINITY;
+    }
+#pragma unroll
+    for (int k = 0; k < kAt; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += exp2_(s[k][e] - z[k]);
   }
   float* w = weights + row * stride + t;
 #pragma unroll
@@ -536,24 +606,24 @@ hipError_t launch_cs(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const v
   const int split_cap = (int)std::max<int64_t>(
       1, std::min<int64_t>(max_splits, num_cus() / ((int64_t)Hkv * n_hchunks)));
   const int64_t slots = ((int64_t)split_cap * Hkv + kXcds - 1) / kXcds * kXcds;
-  // Joining the records takes one block a round trip per eight of them, for each
-  // 1,024 floats of its columns; from five on, groups of splits are joined first
-  // (if there are counters for them).
-  const int64_t floats = (int64_t)std::min(kCols * CS, pairs) * D, turns = (floats + 4 * kThreads - 1) / (4 * kThreads);
-  const int64_t rounds = turns * ((split_cap + 7) / 8) / std::max<int64_t>(1, 4 * kThreads / floats);
-  const int64_t units = (int64_t)B * Hkv * n_hchunks;
-  int group_splits = 0;
-  if (rounds >= 5 && units * (kGroups + 1) <= kDecodeMaxHeads)
-    group_splits = std::max(8, (split_cap + kGroups - 1) / kGroups);
+  // A unit's records are joined by the last of its blocks, which saves a launch,
+  // or by a launch of its own, a block per pair, where one CU would read them for
+  // too long.  In the kernel / apart: one request of 4,097 positions, 4/1 heads,
+  // d = 128 (128 KB) 8.5 / 8.8 us, 16/8 heads of 64 8.0 / 8.7; four of 35,000 15.8 /
+  // 12.8; one of 30,000, 24/4 heads, d = 256 (384 KB) 24.5 / 19.1, three tokens
+  // (1.1 MB) 38.3 / 21.9.
+  const int64_t items = (int64_t)std::min(kCols * CS, pairs) * (D / 4);
+  const int parts = (split_cap + kAt - 1) / kAt;
+  const bool apart = B > 1 || items * 16 * split_cap > 131072;
   const Kv8Workspace at = kv8_workspace(B, sq, Hq, D, max_splits, SUMS ? max_pages * L.page_size : 0);
   uint8_t* base = static_cast<uint8_t*>(ws);
   float* lse = reinterpret_cast<float*>(base + at.lse);
   float* logits = reinterpret_cast<float*>(base + at.logits);
   int shift = 0;
   while ((1 << shift) < L.group_size) ++shift;
-  // the waves' partials; then the ticket and the combine's parts
-  const size_t lds = std::max<size_t>(sizeof(float) * kWaves * std::min(kCols * CS, pairs) * (D + 4),
-                                      16 + kThreads * 24);
+  // the waves' partials; then the ticket and the records' parts
+  const size_t lds = std::max<size_t>(sizeof(float) * kWaves * std::min(kCols, pairs) * (D + 4),
+                                      16 + (apart ? 0 : items * parts * kPartBytes));
   const auto kernel = kv8_decode_kernel<D, BF16, SUMS, CS>;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
@@ -568,10 +638,16 @@ hipError_t launch_cs(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const v
                      lens, reinterpret_cast<uint32_t*>(base),
                      reinterpret_cast<float*>(base + at.records), lse, logits,
                      static_cast<uint16_t*>(out), Hq, sq, Hkv, L.page_size, shift, L.num_pages,
-                     max_pages, max_splits, split_cap, n_hchunks, group_splits, scale * 1.44269504088896340736f);
+                     max_pages, max_splits, split_cap, n_hchunks, apart, scale * 1.44269504088896340736f);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !SUMS) return e;
   const int cap = max_pages * L.page_size;
+  if (e == hipSuccess && apart && split_cap > 1) {
+    hipLaunchKernelGGL((kv8_join_kernel<D, BF16, SUMS, CS>), dim3(pairs, Hkv, B), dim3(kThreads),
+                       D / 4 * parts * kPartBytes, stream, reinterpret_cast<const float*>(base + at.records), lens, lse,
+                       static_cast<uint16_t*>(out), Hq, sq, cap, max_splits, split_cap);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || !SUMS) return e;
   hipLaunchKernelGGL(kv8_sums_kernel, dim3((uint32_t)((cap + 1023) / 1024), Hkv, B), dim3(256), 0,
                      stream, logits, lse, lens, weights, stride, pairs, cap);
   return hipGetLastError();

@@ -161,6 +161,30 @@ def test_decode_of_one_request_is_the_same_in_any_batch():
         assert torch.equal(decode(p, q[b:b + 1], tables[b:b + 1], lens[b:b + 1], 0.1)[0], whole[b])
 
 
+@pytest.mark.parametrize("hq,d,block,bf16,sq", [(4, 128, 64, False, 1), (2, 64, 16, True, 1),
+                                                (4, 256, 32, True, 1), (6, 256, 64, False, 3),
+                                                (9, 128, 32, False, 2), (5, 64, 64, False, 4)])
+def test_decode_of_many_splits_alone_and_in_a_batch(hq, d, block, bf16, sq):
+    """Requests of more than 16 splits, of one and of none; the same bits alone."""
+    rng = np.random.default_rng(hq * sq)
+    lens = [3601, 0, 90, 2900]
+    p = Pair(128, 1, d, block, 60, bf16)
+    tables, _ = tables_for(rng, 128, lens, 60)
+    p.fill(rng, lens, tables)
+    q = rows(rng, 4 * sq, hq, d, bf16, 0.7).view(4, sq, hq, d)
+    cap = tables.shape[1] * 128
+    w = torch.zeros(4, 1, cap, device="cuda")
+    out = decode(p, q, tables, lens, d ** -0.5, weights=w)
+    for b, n in enumerate(lens):
+        r = ref.attend(p.host, wide(q[b]), tables[b], n, d ** -0.5)
+        check_out(out[b], r, d, bf16, "request %d" % b)
+        check_weights(w[b, :, :n].cpu().numpy(), np.zeros((1, n), np.float32), r["weights"], r, d, n,
+                      sq * hq)
+        w1 = torch.zeros(1, 1, cap, device="cuda")
+        alone = decode(p, q[b:b + 1], tables[b:b + 1], lens[b:b + 1], d ** -0.5, weights=w1)
+        assert torch.equal(alone[0], out[b]) and torch.equal(w1[0], w[b])
+
+
 @pytest.mark.parametrize("scale", [0.3, -0.3, 0.0, 1e-30])
 def test_decode_scales(scale):
     rng = np.random.default_rng(2)
