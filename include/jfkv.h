@@ -600,10 +600,13 @@ jf_status jf_tq4_reconstruct(const jf_kv_layout* layout, const void* k_words,
  *
  * Types: k_new, v_new, q and out are fp16 (JF_F16) or bf16 (JF_BF16), one type
  * per call; products run on the matrix cores with fp32 accumulation, codes
- * enter them exactly, softmax statistics and sums are fp32.  Every function
+ * enter them exactly, softmax statistics and sums are fp32.  q must be finite, and
+ * softmax_scale * q . k below 2^126 in magnitude.  Outputs must overlap neither
+ * inputs nor workspaces.  Every function
  * returns JF_ERR_UNSUPPORTED for a geometry, type or size that is not
  * implemented and JF_ERR_INVALID for NULL or misaligned pointers, bad sizes, a
- * short workspace or a non-finite scale; nothing is launched then. */
+ * short workspace or a scale that is not finite or not below 2^126 in magnitude;
+ * nothing is launched then. */
 typedef enum { JF_F16 = 0, JF_BF16 = 1 } jf_dtype;
 
 /* Bytes of one codes array and of one exponent array (the same for K and V). */
@@ -712,7 +715,7 @@ jf_status jf_kv8_attn_weights(const jf_kv_layout* layout,
  * old pages.
  *   weights       fp32 [B][Hkv][weights_stride] (device), as added up by the
  *                 calls above; weights_stride >= max_pages * page_size
- *   keep, recent  keep >= 1, 0 <= recent <= keep
+ *   keep, recent  1 <= keep < 2^30, 0 <= recent <= keep
  *   dst_tables    int32 [B][dst_max_pages] (device), keep <= dst_max_pages *
  *                 page_size; its pages must be none of the source pages, and
  *                 distinct.  Positions on a page ID outside [0, num_pages) are not

@@ -445,7 +445,7 @@ hipError_t launch_kv8_evict(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, 
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid(2u * (uint32_t)((keep + block - 1) / block), L.num_kv_heads, B);
+  const dim3 grid(2u * (uint32_t)((std::min(keep, cap) + block - 1) / block), L.num_kv_heads, B);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<uint8_t*>(pool.k_codes),
                        static_cast<uint8_t*>(pool.k_meta), static_cast<uint8_t*>(pool.v_codes),

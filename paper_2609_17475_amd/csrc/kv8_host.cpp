@@ -1,5 +1,6 @@
 // C entry points of the 8-bit cache: argument validation and dispatch.  A call
 // that fails validation launches nothing.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -53,7 +54,9 @@ jf_status check_dtype(int32_t dtype) {
 bool misaligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) != 0; }
 
 jf_status check_scale(float s) {
-  if (!std::isfinite(s)) return fail(JF_ERR_INVALID, "softmax_scale must be finite");
+  // (times log2 e it has to stay finite)
+  if (!(std::fabs(s) < 0x1p126f))
+    return fail(JF_ERR_INVALID, "softmax_scale must be finite and below 2^126 in magnitude");
   return JF_OK;
 }
 
@@ -78,11 +81,12 @@ jf_status check_chunk(const jf_kv_layout* L, int32_t T, int32_t num_q_heads, int
   if (T < 0 || prefix_len < 0) return fail(JF_ERR_INVALID, "negative size");
   jf_status st = check_heads(L, num_q_heads);
   if (st) return st;
+  if ((int64_t)T * num_q_heads > INT32_MAX || (int64_t)T * num_q_heads * (L->head_dim / 4) > kMaxThreads)
+    return fail(JF_ERR_UNSUPPORTED, "T * num_q_heads too large for one launch");
   if ((int64_t)prefix_len + T > INT32_MAX - 16384)
     return fail(JF_ERR_INVALID, "prefix_len + T overflows int32");
-  if ((int64_t)T * num_q_heads > INT32_MAX || (int64_t)T * num_q_heads * (L->head_dim / 4) > kMaxThreads ||
-      ((int64_t)prefix_len + T + 255) * L->num_kv_heads * 2 > kMaxThreads)
-    return fail(JF_ERR_UNSUPPORTED, "T * num_q_heads or the positions of all KV heads too large for one launch");
+  if (((int64_t)prefix_len + T + 255) * L->num_kv_heads * 2 > kMaxThreads)
+    return fail(JF_ERR_UNSUPPORTED, "the positions of all KV heads are too many for one launch");
   return JF_OK;
 }
 
@@ -275,6 +279,11 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool, 
                 layout->page_size);
   if ((int64_t)B * layout->num_kv_heads * 256 > kMaxThreads)
     return fail(JF_ERR_UNSUPPORTED, "B * num_kv_heads too large for one launch");
+  // blocks of the positions that can stay, K's and V's, of 256 threads at most;
+  // and room for the strides of loops that count to keep in 32 bits
+  const int64_t most = std::min<int64_t>(keep, (int64_t)max_pages * layout->page_size);
+  if (keep > INT32_MAX / 2 || (most / layout->group_size + 1) * 2 * 256 > kMaxThreads)
+    return fail(JF_ERR_UNSUPPORTED, "keep %d too large for one launch", keep);
   if (!block_tables || !seq_lens || !weights || !dst_tables || !kept || !kept_weights ||
       (need && !workspace))
     return fail(JF_ERR_INVALID, "NULL device pointer");

@@ -145,3 +145,16 @@ def test_pool_bytes():
     assert jfkv.kv8_pool_bytes(jfkv.layout(256, 8, 128, 64, 10)) == (10 * 8 * 256 * 128, 10 * 8 * 4)
     with pytest.raises(jfkv.JfError):
         jfkv.kv8_pool_bytes(jfkv.layout(256, 8, 96, 64, 10))
+
+
+def test_evict_counts_that_32_bits_do_not_hold():
+    for change in ({"keep": 1 << 30, "dst_pages": 1 << 23},
+                   {"layout": (256, 8, 128, 16, 16), "keep": 1 << 28, "dst_pages": 1 << 20,
+                    "max_pages": 1 << 20, "stride": 1 << 28}):
+        assert _call(L.jf_kv8_evict, EVICT, change) == UNSUPPORTED, change
+
+
+@pytest.mark.parametrize("fn,spec", CALLS[1:4], ids=lambda x: getattr(x, "__name__", ""))
+def test_scales_that_overflow_in_base_two(fn, spec):
+    for scale in (3e38, -3e38, 2.0 ** 126):
+        assert _call(fn, spec, {"scale": scale}) == INVALID
