@@ -671,6 +671,185 @@ __global__ __launch_bounds__(kWThreads, NS > 2 ? 2 : 3) void kv8_weights_kernel(
   if (n < 4 * NS && pos < L) weights[(size_t)kv * stride + pos] += v[0];
 }
 
+// The same where all columns' queries fit into LDS (an observation window): they
+// are brought there once, and a block per CU walks over the positions of its KV
+// head, each wave over its own 64 at a time without a barrier, the next ones' K on
+// the way meanwhile.
+constexpr int kWinWaves = 8;
+constexpr int kWinThreads = 64 * kWinWaves;
+constexpr int kWinNS = 4;
+template <int D>
+constexpr size_t window_bytes(int64_t ncols) {  // (whole pairs of groups of 16)
+  return (size_t)((ncols + 31) / 32 * 32) * (2 * D + 8);
+}
+constexpr size_t kWindowMax = 147456;
+
+template <int D, bool BF16>
+__global__ __launch_bounds__(kWinThreads) void kv8_window_weights_kernel(
+    const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
+    const uint16_t* __restrict__ q, const float* __restrict__ lse,
+    const int32_t* __restrict__ table, float* __restrict__ weights, int64_t stride, int Hq, int Hkv,
+    int P, int block_shift, int num_pages, int T, int prefix, float scale_log2, uint32_t flip) {
+  constexpr int C = D / 64, NS = kWinNS;
+  constexpr bool kAheadK = D <= 128;  // (the registers do not hold two sets of d = 256)
+  extern __shared__ __align__(16) u32x4 qs[];  // [16 columns][c][half][lane], lse, row
+  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kv = blockIdx.x % Hkv, gq = Hq / Hkv, ncols = T * gq, pairs = (ncols + 31) / 32;
+  float* const s_lse = reinterpret_cast<float*>(qs + pairs * 32 * (D / 8));
+  int* const s_row = reinterpret_cast<int*>(s_lse + pairs * 32);
+  const int L = prefix + T, units = (L + 16 * NS - 1) / (16 * NS);
+  const int stepu = gridDim.x / Hkv * kWinWaves;
+  const int last = units - 1;
+
+  u32x4 kc[NS][C];
+  uint32_t ke[NS];
+  auto page_of = [&](int u) JF_INLINE { return table[min(u, last) * (16 * NS) / P]; };
+  auto fetch = [&](int u, int pid) JF_INLINE {
+    const size_t run = (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv;
+    const int slot0 = min(u, last) * (16 * NS) % P;
+#pragma unroll
+    for (int t = 0; t < NS; ++t) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        kc[t][c] = *reinterpret_cast<const u32x4*>(k_codes + (run * P + slot0 + 16 * t + n) * D +
+                                                   64 * c + 16 * g);
+      ke[t] = k_exps[run * (P >> block_shift) + ((slot0 + 16 * t) >> block_shift)];
+    }
+  };
+  int u = blockIdx.x / Hkv * kWinWaves + wave;
+  int pid = page_of(u), pid_next = page_of(u + stepu);
+  if (kAheadK) fetch(u, pid);
+
+  // ---- all columns to LDS; those past the end weigh nothing
+  const int count = pairs * 32 * (D / 8);
+  for (int i0 = tid; i0 < count; i0 += 8 * kWinThreads) {
+    u32x4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = min(i0 + k * kWinThreads, count - 1), col = min(i / (128 * C) * 16 + i % 16, ncols - 1);
+      x[k] = *reinterpret_cast<const u32x4*>(
+          q + ((size_t)(col / gq) * Hq + kv * gq + col % gq) * D + i / 128 % C * 64 +
+          i % 64 / 16 * 16 + i / 64 % 2 * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (i0 + k * kWinThreads < count) qs[i0 + k * kWinThreads] = x[k] ^ flip;
+  }
+  for (int col = tid; col < pairs * 32; col += kWinThreads) {
+    const int row = min(col, ncols - 1) / gq;
+    const float z = lse[(size_t)row * Hq + kv * gq + min(col, ncols - 1) % gq];
+    s_lse[col] = col < ncols && z != -INFINITY ? z * kLog2e : INFINITY;
+    s_row[col] = row;
+  }
+  __syncthreads();
+
+  // ---- 32 columns against the wave's positions: the products of one pair of
+  // groups, and between them the exponentials of the pair before
+  struct Scores {
+    f32x4 s[2][NS];
+    float z[2];
+  };
+  u32x4 kf[NS][C][2];
+  float f[NS], w[NS][4];
+  auto one = [&](const Scores& a, int i) JF_INLINE {  // score i of 32
+    const int h = i / (4 * NS), t = i / 4 % NS, e = i % 4;
+    w[t][e] += exp2_(fmaf(a.s[h][t][e], f[t], -a.z[h]));
+  };
+  auto weigh = [&](const Scores& a) JF_INLINE {
+#pragma unroll
+    for (int i = 0; i < 8 * NS; ++i) one(a, i);
+  };
+  auto step = [&](int p, Scores& now, const Scores& before, auto both) JF_INLINE {
+    constexpr int kOps = 4 * C, kAhead = 4, kPer = 8 * NS / kOps;
+    const u32x4* const from = qs + p * 32 * (D / 8) + lane;
+    u32x4 ring[kAhead];
+#pragma unroll
+    for (int o = 0; o < kAhead; ++o) ring[o] = from[o * 64];
+    now.z[0] = s_lse[32 * p + n], now.z[1] = s_lse[32 * p + 16 + n];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < NS; ++t) now.s[h][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int o = 0; o < kOps; ++o) {  // (in the order of LDS: [h][c][half])
+      const u32x4 x = ring[o % kAhead];
+      if (o + kAhead < kOps) ring[o % kAhead] = from[(o + kAhead) * 64];
+      const int h = o / (2 * C), c = o / 2 % C, j = o % 2;
+#pragma unroll
+      for (int t = 0; t < NS; ++t) now.s[h][t] = mma<BF16>(kf[t][c][j], x, now.s[h][t]);
+      if constexpr (decltype(both)::value) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) one(before, o * kPer + i);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  Scores scored, spare;
+
+  for (; u < units; u += stepu) {
+    if (!kAheadK) fetch(u, pid);
+    const int key0 = u * (16 * NS), pos = key0 + 16 * (n / 4) + 4 * g + n % 4;
+    const float old = weights[(size_t)kv * stride + min(pos, L - 1)];
+    const bool on = (uint32_t)pid < (uint32_t)num_pages;
+#pragma unroll
+    for (int t = 0; t < NS; ++t) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        kf[t][c][0] = widen8<BF16>(kc[t][c].x, kc[t][c].y);
+        kf[t][c][1] = widen8<BF16>(kc[t][c].z, kc[t][c].w);
+      }
+      // (not 0, so that a hidden score times it stays -inf)
+      f[t] = fmaxf(scale_log2 * power2((int)ke[t] - 127), 1e-37f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[t][i] = 0.0f;
+    }
+    pid = pid_next;
+    if (kAheadK) fetch(u + stepu, pid);
+    pid_next = page_of(u + 2 * stepu);
+    if (!on) continue;
+    if (key0 + 16 * NS - 1 > prefix) {  // (some rows do not see all of these positions)
+      for (int p = 0; p < pairs; ++p) {
+        step(p, scored, spare, std::false_type{});
+        const int see0 = prefix + s_row[32 * p + n], see1 = prefix + s_row[32 * p + 16 + n];
+#pragma unroll
+        for (int t = 0; t < NS; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int pos = key0 + 16 * t + 4 * g + i;
+            if (pos > see0) scored.s[0][t][i] = -INFINITY;
+            if (pos > see1) scored.s[1][t][i] = -INFINITY;
+          }
+        weigh(scored);
+      }
+    } else {
+      step(0, scored, spare, std::false_type{});
+      int p = 1;
+      for (; p + 1 < pairs; p += 2) {
+        step(p, spare, scored, std::true_type{});
+        step(p + 1, scored, spare, std::true_type{});
+      }
+      if (p < pairs) {
+        step(p, spare, scored, std::true_type{});
+        weigh(spare);
+      } else {
+        weigh(scored);
+      }
+    }
+    float v[4 * NS];  // (as above: lane n gets the sum of its position)
+#pragma unroll
+    for (int i = 0; i < 4 * NS; ++i) v[i] = w[i / 4][i % 4];
+#pragma unroll
+    for (int o = 2 * NS; o; o >>= 1)
+#pragma unroll
+      for (int k = 0; k < o; ++k) {
+        const bool up = (n & o) != 0;
+        v[k] = (up ? v[k + o] : v[k]) + __shfl_xor(up ? v[k] : v[k + o], o);
+      }
+    if (pos < L) weights[(size_t)kv * stride + pos] = old + v[0];
+  }
+}
+
 template <int D, bool BF16>
 hipError_t launch_prefill_t(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q,
                             int32_t T, int32_t Hq, const int32_t* table, int32_t prefix,
@@ -743,6 +922,41 @@ hipError_t launch_kv8_prefill(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool
 }
 
 namespace {
+// Windows whose queries fit into LDS, where every wave has a unit of positions to
+// walk over (d = 256, where K is not fetched ahead: two).  64 rows, 32/8 heads of
+// 128, over 262,080 positions 219 -> 173 us, 65,472 62 -> 55, 16,000 18.5 -> 17, but
+// 8,000 11 -> 18; 40 rows, 24/4 heads of 256, over 200,000 138 -> 117, but 30,000
+// 25 -> 27.  At d = 64 (100,000 positions of 16/2 heads, 128 rows: 60 both) the
+// vector work decides, which is the same.
+template <int D>
+bool window_takes(const jf_kv_layout& L, int32_t T, int32_t Hq, int64_t keys) {
+  const int64_t units = keys / (16 * kWinNS) * L.num_kv_heads;
+  return window_bytes<D>((int64_t)T * (Hq / L.num_kv_heads)) <= kWindowMax &&
+         units >= (D > 128 ? 2 : 1) * (int64_t)(num_cus() / L.num_kv_heads * L.num_kv_heads) * kWinWaves * 31 / 32;
+}
+
+template <int D, bool BF16>
+hipError_t launch_window_t(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q,
+                           const float* lse, int32_t T, int32_t Hq, const int32_t* table,
+                           int32_t prefix, float scale, float* weights, int64_t stride,
+                           hipStream_t stream) {
+  const auto kernel = kv8_window_weights_kernel<D, BF16>;
+  const size_t lds = window_bytes<D>((int64_t)T * (Hq / L.num_kv_heads));
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  const int blocks = std::max(num_cus() / L.num_kv_heads, 1) * L.num_kv_heads;
+  hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kWinThreads), lds, stream,
+                     static_cast<const uint8_t*>(pool.k_codes),
+                     static_cast<const uint8_t*>(pool.k_meta), static_cast<const uint16_t*>(q), lse,
+                     table, weights, stride, Hq, L.num_kv_heads, L.page_size,
+                     shift_of(L.group_size), L.num_pages, T, prefix, std::fabs(scale) * kLog2e,
+                     scale < 0.0f ? 0x80008000u : 0u);
+  return hipGetLastError();
+}
+
 template <int D, bool BF16, int NS>
 hipError_t launch_weights_t(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const void* q,
                             const float* lse, int32_t T, int32_t Hq, const int32_t* table,
@@ -769,12 +983,16 @@ hipError_t launch_kv8_weights(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool
   // Few columns over many positions: 64 positions per wave, for fewer starts; else
   // 32, for an even chip.  64 rows, 32/8 heads of 128, 65,472 positions 57 us
   // against 72, 24/4 heads of 256, 30,000 34 against 44; but 8,000 positions 14.3
-  // against 12.7, and 2,048 rows without a prefix 188 against 134.
+  // against 12.7, and 2,048 rows without a prefix 188 against 134.  (Measured before
+  // windows had a kernel of their own.)
   const int64_t keys = (int64_t)prefix_len + T;
   const bool four = (int64_t)T * (Hq / L.num_kv_heads) <= 1024 &&
                     keys / 256 * L.num_kv_heads >= num_cus() * 3 / 2;
 #define JF_CASE(D_)                                                                          \
   if (L.head_dim == D_) {                                                                    \
+    if constexpr (D_ > 64)                                                                   \
+      if (window_takes<D_>(L, T, Hq, keys))                                                  \
+        return bf16 ? go(launch_window_t<D_, true>) : go(launch_window_t<D_, false>);        \
     if (four) return bf16 ? go(launch_weights_t<D_, true, 4>) : go(launch_weights_t<D_, false, 4>); \
     return bf16 ? go(launch_weights_t<D_, true, 2>) : go(launch_weights_t<D_, false, 2>);    \
   }

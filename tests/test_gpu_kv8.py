@@ -329,6 +329,64 @@ def test_prefill_and_its_weights(P, hkv, hq, d, block, bf16, T, prefix):
         check_weights(part.cpu().numpy(), np.zeros((hkv, n)), rw["weights"], rw, d, n, 3 * hq // hkv)
 
 
+def window(host, q, table, n, scale, first):
+    """As ref.attend, all rows of a head at once: lse, the weights that rows first ..
+    add, and the largest scale * sum |q k|."""
+    T, hq, d = q.shape
+    g = hq // host.hkv
+    lse, weights, dots = np.empty((T, hq)), np.zeros((host.hkv, n)), 0.0
+    sees = np.arange(n)[:, None] <= n - T + np.arange(T)[None, :]
+    for h in range(host.hkv):
+        k, ok = host.values(0, table, n, h)
+        k = np.where(ok[:, None], k, 0.0)
+        for j in range(h * g, h * g + g):
+            z = np.where(sees & ok[:, None], scale * (k @ q[:, j].T), -np.inf)
+            dots = max(dots, float(np.max(abs(scale) * (np.abs(k) @ np.abs(q[:, j]).T))))
+            top = z.max(0)
+            lse[:, j] = top + np.log(np.exp(z - top).sum(0))
+            weights[h] += np.exp(z - lse[:, j])[:, first:].sum(1)
+    return lse, weights, dots
+
+
+@pytest.mark.parametrize("P,hkv,hq,d,block,bf16,T,n,scale", [
+    (256, 8, 16, 128, 64, False, 3, 16301, 0.05),     # one pair of column groups
+    (256, 8, 16, 128, 32, True, 37, 16384, 0.05),     # three, the last half empty
+    (64, 3, 9, 128, 16, False, 64, 42331, -0.05),     # heads that the chip's count is no multiple of
+    (256, 16, 48, 256, 32, True, 11, 16140, 0.03),
+])
+def test_weights_of_a_window_over_many_positions(P, hkv, hq, d, block, bf16, T, n, scale):
+    rng = np.random.default_rng(n)
+    pages = -(-n // P) + 2
+    p = Pair(P, hkv, d, block, pages, bf16)
+    for which in range(2):
+        c = rng.integers(0, 256, p.host.codes[which].shape, np.uint8)
+        c[(c & 127) == 127] = 0
+        p.host.codes[which][...] = c
+        p.host.exps[which][...] = rng.integers(117, 121, p.host.exps[which].shape)
+    tables, _ = tables_for(rng, P, [n], pages)
+    tables[0, 5] = pages
+    page, slot = tables[0, (n - 1) // P], (n - 1) % P + 1
+    p.host.codes[0][page, :, slot:] = STALE  # slots not written yet
+    for name, data in zip(("k_codes", "k_exps", "v_codes", "v_exps"), p.host.pool_bytes()):
+        getattr(p.gpu, name).copy_(torch.from_numpy(np.ascontiguousarray(data)))
+    q = rows(rng, T, hq, d, bf16, 0.3)
+    before = rng.random((hkv, n + 3)).astype(np.float32)
+    for hidden in (0, 1):  # (rows that saw nothing add nothing)
+        z, added, dots = window(p.host, wide(q), tables[0], n, scale, hidden)
+        lse = torch.from_numpy(z.astype(np.float32)).cuda()
+        lse[:hidden] = -float("inf")
+        w = torch.from_numpy(before).cuda()
+        jfkv.jf_kv8_attn_weights(p.gpu, q.cuda(), lse, i32(tables[0]), n - T, scale, w)
+        got = w.cpu().numpy()
+        # (twice the scores' error: the lse's own rounding beside it)
+        check_weights(got[:, :n], before[:, :n], added, dict(dots=2 * dots), d, n, T * hq // hkv)
+        assert np.array_equal(got[:, n:], before[:, n:])
+        assert np.array_equal(got[:, 5 * P:6 * P], before[:, 5 * P:6 * P])
+        again = torch.from_numpy(before).cuda()
+        jfkv.jf_kv8_attn_weights(p.gpu, q.cuda(), lse, i32(tables[0]), n - T, scale, again)
+        assert torch.equal(w, again)
+
+
 @pytest.mark.parametrize("split", [False, True])
 def test_prefill_passes_over_pages_outside_the_pool(split):
     rng = np.random.default_rng(4)
