@@ -602,6 +602,153 @@ def test_captured_step_replays_like_the_eager_one():
                 assert torch.equal(a, b)
 
 
+def random_pool(rng, P, hkv, d, block, pages):
+    """A pool of random finite codes and small exponents, unlike any appended one."""
+    pool = jfkv.KV8Pool(jfkv.layout(P, hkv, d, block, pages))
+    for t in (pool.k_codes, pool.v_codes):
+        c = rng.integers(0, 256, t.numel(), np.uint8)
+        c[(c & 127) == 127] = 0
+        t.copy_(torch.from_numpy(c))
+    for t in (pool.k_exps, pool.v_exps):
+        t.copy_(torch.from_numpy(rng.integers(117, 121, t.numel()).astype(np.uint8)))
+    return pool
+
+
+def long_calls(pool, rng, P, hkv, hq, d, n, keep, dst, stream=None):
+    """Calls that take the larger launches (records joined apart, eviction in parts,
+    a window's weights where the chip is filled), and what they write."""
+    s = dict(stream=stream)
+    pages = -(-n // P)
+    t, lens = i32(np.stack([np.arange(pages), np.arange(pages)[::-1]])), i32([n, n - 77])
+    q = rows(rng, 6, hq, d, True, 0.5).view(2, 3, hq, d).cuda()
+    qs = rows(rng, 9, hq, d, True, 0.5).cuda()
+    out, outs = torch.empty_like(q), torch.empty_like(qs)
+    lse = torch.empty(9, hq, device="cuda")
+    w = torch.zeros(2, hkv, pages * P, device="cuda")
+    kept = torch.empty(2, hkv, keep, dtype=torch.int32, device="cuda")
+    kept_w = torch.empty(2, hkv, keep, device="cuda")
+    ws = torch.zeros(jfkv.jf_kv8_decode_workspace_bytes(pool.layout, 2, 3, hq, 64, pages),
+                     dtype=torch.uint8, device="cuda")
+    ws2, ws3 = (torch.empty(max(16, b), dtype=torch.uint8, device="cuda") for b in (
+        jfkv.jf_kv8_prefill_workspace_bytes(pool.layout, 9, hq, n - 9),
+        jfkv.jf_kv8_evict_workspace_bytes(pool.layout, 2, pages, keep)))
+    calls = [jfkv.bind_kv8_decode(pool, q, t, lens, 0.03, 64, ws, out, weights=w, **s),
+             jfkv.bind_kv8_prefill(pool, qs, t[0], n - 9, 0.03, outs, lse=lse, workspace=ws2, **s),
+             jfkv.bind_kv8_attn_weights(pool, qs, lse, t[0], n - 9, 0.03, w[0], **s),
+             jfkv.bind_kv8_evict(pool, t, lens, w, keep, 50, i32(dst), ws3, kept, kept_w, **s)]
+    return calls, w, (out, outs, lse, w, kept, kept_w)
+
+
+def dst_bytes(pool, pages):
+    lay = pool.layout
+    n = lay.num_kv_heads * lay.page_size
+    return [t.view(-1, n * lay.head_dim // per)[pages].clone() for t, per in (
+        (pool.k_codes, 1), (pool.v_codes, 1), (pool.k_exps, lay.head_dim * lay.group_size),
+        (pool.v_exps, lay.head_dim * lay.group_size))]
+
+
+@pytest.mark.parametrize("d,hkv,hq", [(256, 8, 48), (128, 8, 56)])
+def test_captured_long_calls_replay_like_eager_ones(d, hkv, hq):
+    rng = np.random.default_rng(d)
+    P, n, keep = 256, 33000 if d > 128 else 17000, 700
+    pages = -(-n // P)
+    pool = random_pool(rng, P, hkv, d, 32, pages + 6)
+    dst = np.arange(pages, pages + 6).reshape(2, 3)
+    side = torch.cuda.Stream()
+    calls, w, results = long_calls(pool, rng, P, hkv, hq, d, n, keep, dst, side)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for c in calls:
+            c()
+        side.synchronize()
+        want = [t.clone() for t in results] + dst_bytes(pool, slice(pages, None))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            w.zero_()
+            for c in calls:
+                c()
+    for turn in range(3):
+        for run in (g.replay, None):
+            for t in results:
+                t.fill_(1)
+            torch.cuda.synchronize()
+            if run:
+                run()
+            else:
+                with torch.cuda.stream(side):
+                    w.zero_()
+                    for c in calls:
+                        c()
+            torch.cuda.synchronize()
+            for a, b in zip(list(results) + dst_bytes(pool, slice(pages, None)), want):
+                assert torch.equal(a, b)
+
+
+def test_two_sets_of_calls_at_once():
+    """Two streams over one pool, each with its own workspaces and pages to move to."""
+    rng = np.random.default_rng(6)
+    P, hkv, hq, d, n, keep = 256, 8, 48, 128, 17000, 700
+    pages = -(-n // P)
+    pool = random_pool(rng, P, hkv, d, 64, pages + 12)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sets = [long_calls(pool, rng, P, hkv, hq, d, n, keep,
+                       np.arange(pages + 6 * i, pages + 6 * i + 6).reshape(2, 3), st)
+            for i, st in enumerate(streams)]
+    torch.cuda.synchronize()
+    want = None
+    for alone in (True, False, False):
+        for (calls, w, results), st in zip(sets, streams):
+            w.zero_()
+        torch.cuda.synchronize()
+        for i in range(len(sets[0][0])):
+            for calls, w, results in sets:
+                calls[i]()
+                if alone:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        got = [t.clone() for _, _, r in sets for t in r] + dst_bytes(pool, slice(pages, None))
+        if want is None:
+            want = got
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def test_pages_beyond_four_gibibytes():
+    """The last pages of a pool whose arrays pass 2^32 bytes, against a small pool."""
+    rng = np.random.default_rng(8)
+    P, hkv, hq, d, block = 1024, 8, 16, 256, 64
+    small = random_pool(rng, P, hkv, d, block, 8)
+    first = (1 << 32) // (P * hkv * d) + 3
+    big = jfkv.KV8Pool(jfkv.layout(P, hkv, d, block, first + 8))
+    for name in ("k_codes", "k_exps", "v_codes", "v_exps"):
+        a, b = getattr(small, name), getattr(big, name)
+        b[b.numel() - a.numel():].copy_(a)
+    n = 5 * P + 100
+    k, v = (rows(rng, 200, hkv, d, True).cuda() for _ in range(2))
+    q = rows(rng, 2, hq, d, True, 0.3).view(1, 2, hq, d).cuda()
+    qs = rows(rng, 70, hq, d, True, 0.3).cuda()
+    w0 = torch.from_numpy(rng.random((1, hkv, 6 * P)).astype(np.float32)).cuda()
+    got = []
+    for pool, at in ((small, 0), (big, first)):
+        t, dst = i32([[at + i for i in (4, 0, 5, 2, 1, 3)]]), i32([[at + 7, at + 6]])
+        jfkv.jf_kv8_append(pool, k, v, i32([0, 200]), i32([n - 200]), t)
+        w = w0.clone()
+        ws = torch.zeros(jfkv.jf_kv8_decode_workspace_bytes(pool.layout, 1, 2, hq, 64, 6),
+                         dtype=torch.uint8, device="cuda")
+        out, outs, lse = torch.empty_like(q), torch.empty_like(qs), torch.empty(70, hq, device="cuda")
+        jfkv.jf_kv8_decode_attn(pool, q, t, i32([n]), 0.03, 64, ws, out, weights=w)
+        jfkv.jf_kv8_prefill_attn(pool, qs, t[0], n - 70, 0.03, outs, lse=lse)
+        jfkv.jf_kv8_attn_weights(pool, qs, lse, t[0], n - 70, 0.03, w[0])
+        kept = torch.empty(1, hkv, 1500, dtype=torch.int32, device="cuda")
+        kept_w = torch.empty(1, hkv, 1500, device="cuda")
+        jfkv.jf_kv8_evict(pool, t, i32([n]), w, 1500, 64, dst, None, kept, kept_w)
+        got.append([out, outs, lse, w, kept, kept_w] + dst_bytes(pool, slice(at, None)))
+    torch.cuda.synchronize()
+    assert torch.isfinite(got[0][0]).all() and got[0][0].any()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 def test_python_refusals():
     p = Pair(64, 2, 64, 16, 2)
     q = torch.zeros(1, 1, 4, 64, dtype=torch.float16, device="cuda")
