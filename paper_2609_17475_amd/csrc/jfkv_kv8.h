@@ -115,5 +115,10 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t codes, float f) {
   return encode2<true>(hi.x * f, hi.y * f, encode2<false>(lo.x * f, lo.y * f, 0u));
 }
 
+// The larger of two scores (NaN if one is).  As one instruction for up to three
+// of them: fmaxf first passes each matrix product's result through another, for
+// signalling NaNs.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 }  // namespace kv8
 }  // namespace jfkv

@@ -308,8 +308,9 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 2 : 3) void kv8_decod
     bool raise = false;
 #pragma unroll
     for (int cs = 0; cs < CS; ++cs) {
-      top[cs] = fmaxf(fmaxf(s[cs][0][0], s[cs][0][1]), fmaxf(s[cs][0][2], s[cs][0][3]));
-      top[cs] = fmaxf(top[cs], fmaxf(fmaxf(s[cs][1][0], s[cs][1][1]), fmaxf(s[cs][1][2], s[cs][1][3])));
+      top[cs] = larger(larger(larger(s[cs][0][0], s[cs][0][1]), s[cs][0][2]), s[cs][0][3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top[cs] = larger(top[cs], s[cs][1][i]);
       raise |= top[cs] > m[cs] + kMargin;
     }
     if (__any(raise)) {

@@ -254,8 +254,8 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
       top[cs] = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        top[cs] = fmaxf(top[cs], f[t] * fmaxf(fmaxf(s[t][cs][0], s[t][cs][1]),
-                                              fmaxf(s[t][cs][2], s[t][cs][3])));
+        top[cs] = larger(top[cs], f[t] * larger(larger(larger(s[t][cs][0], s[t][cs][1]),
+                                                       s[t][cs][2]), s[t][cs][3]));
       raise |= top[cs] > m[cs] + kMargin;
     }
     if (__any(raise)) {
