@@ -96,30 +96,37 @@ constexpr int kAt = 8;
 struct Parts {
   f32x4* num;
   f32x2* ml;
-  // the sums of the first `count` of eight records, as part u
-  __device__ __forceinline__ void put(int u, const f32x4 (&o)[kAt], const f32x2 (&r)[kAt],
-                                      int count) const {
-    float m = r[0].x;
+  // m and l of the first `count` of eight records, and the records' factors
+  static __device__ __forceinline__ f32x2 weigh(const f32x2 (&r)[kAt], int count, float (&f)[kAt]) {
+    float m = r[0].x, den = 0.0f;
 #pragma unroll
     for (int k = 1; k < kAt; ++k) m = fmaxf(m, r[k].x);  // (behind count: repeated ones)
-    f32x4 n = {0.0f, 0.0f, 0.0f, 0.0f};
-    float den = 0.0f;
 #pragma unroll
     for (int k = 0; k < kAt; ++k) {
-      const float f = k >= count || r[k].x == -INFINITY ? 0.0f : exp2_(r[k].x - m);
-      n += o[k] * f;
-      den = fmaf(f, r[k].y, den);
+      f[k] = k >= count || r[k].x == -INFINITY ? 0.0f : exp2_(r[k].x - m);
+      den = fmaf(f[k], r[k].y, den);
     }
-    num[u] = n, ml[u] = f32x2{m, den};
+    return f32x2{m, den};
+  }
+  // their sums, as part u
+  __device__ __forceinline__ void put(int u, const f32x4 (&o)[kAt], const f32x2 (&r)[kAt],
+                                      int count) const {
+    float f[kAt];
+    ml[u] = weigh(r, count, f);
+    f32x4 n = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) n += o[k] * f[k];
+    num[u] = n;
   }
   // item i of `items` over all parts
+  template <bool NUM = true>
   __device__ __forceinline__ Joined get(int i, int items, int parts) const {
     Joined a;
     for (int u = 0; u < parts; ++u) a.m = fmaxf(a.m, ml[u * items + i].x);
     for (int u = 0; u < parts; ++u) {
       const f32x2 r = ml[u * items + i];
       const float f = r.x == -INFINITY ? 0.0f : exp2_(r.x - a.m);
-      a.num += num[u * items + i] * f;
+      if (NUM) a.num += num[u * items + i] * f;
       a.den = fmaf(f, r.y, a.den);
     }
     return a;
@@ -521,21 +528,83 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 2 : 3) void kv8_decod
   }
 }
 
+// Adds the weights exp2(s_t - z) of pairs p0 .. p0 + n - 1 (scores lg [pair][cap], z
+// from zs) at four positions.
+__device__ __forceinline__ void add_pairs(f32x4& sum, const float* lg, size_t cap, const float* zs,
+                                          int n) {
+  constexpr int kAhead = 6;  // loads on the way (one: 9.1 us for 6.1 of 78,000 positions, 18 pairs)
+  for (int i0 = 0; i0 < n; i0 += kAhead) {
+    f32x4 s[kAhead];
+    float z[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = min(i0 + k, n - 1);
+      s[k] = *reinterpret_cast<const f32x4*>(lg + (size_t)i * cap);
+      z[k] = i0 + k < n ? zs[i] : INFINITY;
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += exp2_(s[k][e] - z[k]);
+  }
+}
+__device__ __forceinline__ void store_sums(float* w, int64_t t, int L, const f32x4& sum) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (t + e < L) w[t + e] += sum[e];
+}
+
 // The same where a launch of its own joins the records: a workgroup per (request,
-// KV head, pair).
+// KV head, pair).  SUMS: and workgroups behind them for the weights' sums, 1,024
+// positions each, which take the log-sum-exps from the records themselves rather
+// than wait for another launch.
 template <int D, bool BF16, bool SUMS, int CS>
 __global__ __launch_bounds__(kThreads) void kv8_join_kernel(
-    const float* __restrict__ recs, const int32_t* __restrict__ seq_lens, float* __restrict__ lse,
-    uint16_t* __restrict__ out, int Hq, int sq, int cap, int max_splits, int split_cap) {
+    const float* __restrict__ recs, const int32_t* __restrict__ seq_lens,
+    const float* __restrict__ lse, uint16_t* __restrict__ out, const float* __restrict__ logits,
+    float* __restrict__ weights, int64_t stride, int pairs, int Hq, int sq, int cap, int max_splits,
+    int split_cap) {
   constexpr int kPer = D / 4;
   extern __shared__ __align__(16) float smem[];
-  const int pair = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, pairs = gridDim.x, Hkv = gridDim.y;
-  const int S = splits_of<D, CS>(min(max(seq_lens[b], 0), cap), split_cap);
-  if (S == 1) return;  // (the output is there)
+  const int pair = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
+  const int L = min(max(seq_lens[b], 0), cap), S = splits_of<D, CS>(L, split_cap);
   const int tid = threadIdx.x, parts = (S + kAt - 1) / kAt;
-  const size_t rec = ((size_t)b * Hkv + kv) * pairs + pair;
-  const float* const from = recs + rec * max_splits * (D + 4);
+  const size_t row = (size_t)b * Hkv + kv;
   const Parts at = parts_at(smem, kPer * parts);
+  if (SUMS && pair >= pairs) {
+    constexpr int kChunk = 32;  // pairs at a time
+    f32x2* const ml = reinterpret_cast<f32x2*>(smem);        // [part][pair]
+    float* const zs = reinterpret_cast<float*>(ml + kChunk * parts);
+    const int64_t t0 = (int64_t)(pair - pairs) * (4 * kThreads), t = t0 + 4 * tid;
+    if (t0 >= L) return;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p0 = 0; p0 < pairs; p0 += kChunk) {
+      const int n = min(kChunk, pairs - p0);
+      if (S == 1) {
+        if (tid < n) zs[tid] = lse[row * pairs + p0 + tid];
+      } else {
+        for (int u = tid; u < n * parts; u += kThreads) {
+          const int s0 = u / n * kAt;
+          const float* const from = recs + (row * pairs + p0 + u % n) * max_splits * (D + 4) + D;
+          f32x2 r[kAt];
+          float f[kAt];
+#pragma unroll
+          for (int k = 0; k < kAt; ++k)
+            r[k] = *reinterpret_cast<const f32x2*>(from + (size_t)min(s0 + k, S - 1) * (D + 4));
+          ml[u] = Parts::weigh(r, S - s0, f);
+        }
+        __syncthreads();
+        if (tid < n) zs[tid] = Parts{nullptr, ml}.template get<false>(tid, n, parts).lse();
+      }
+      __syncthreads();
+      if (t < L) add_pairs(sum, logits + (row * pairs + p0) * (size_t)cap + t, cap, zs, n);
+      __syncthreads();
+    }
+    store_sums(weights + row * stride, t, L, sum);
+    return;
+  }
+  if (S == 1) return;  // (the output is there)
+  const float* const from = recs + (row * pairs + pair) * max_splits * (D + 4);
   for (int u = tid; u < kPer * parts; u += kThreads) {
     const int s0 = u / kPer * kAt;
     f32x4 o[kAt];
@@ -551,47 +620,27 @@ __global__ __launch_bounds__(kThreads) void kv8_join_kernel(
   __syncthreads();
   if (tid >= kPer) return;
   const int gq = Hq / Hkv;
-  const Joined sum = at.get(tid, kPer, parts);
-  const f32x4 r = sum.out();
+  const f32x4 r = at.get(tid, kPer, parts).out();
   uint16_t* op = out + (((size_t)b * sq + pair / gq) * Hq + kv * gq + pair % gq) * D + 4 * tid;
   *reinterpret_cast<uint2*>(op) = make_uint2(narrow2<BF16>(r.x, r.y), narrow2<BF16>(r.z, r.w));
-  if (SUMS && tid == 0) lse[rec] = sum.lse();
 }
 
-// weights[b][kv][t] += sum over the pairs of exp2(s_t - lse): the decode left
-// the scores (log2 units) and the log-sum-exps of its pairs.  Four positions
+// weights[b][kv][t] += sum over the pairs of exp2(s_t - lse) where the decode itself
+// left the log-sum-exps of its pairs (and the scores, log2 units).  Four positions
 // per thread; positions from the request's length on are left as they are.
-__global__ __launch_bounds__(256) void kv8_sums_kernel(const float* __restrict__ logits,
-                                                       const float* __restrict__ lse,
-                                                       const int32_t* __restrict__ seq_lens,
-                                                       float* __restrict__ weights, int64_t stride,
-                                                       int pairs, int cap) {
+__global__ __launch_bounds__(kThreads) void kv8_sums_kernel(const float* __restrict__ logits,
+                                                            const float* __restrict__ lse,
+                                                            const int32_t* __restrict__ seq_lens,
+                                                            float* __restrict__ weights,
+                                                            int64_t stride, int pairs, int cap) {
   const int b = blockIdx.z, kv = blockIdx.y, Hkv = gridDim.y;
   const int L = min(max(seq_lens[b], 0), cap);
-  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * 4;
   if (t >= L) return;
   const size_t row = (size_t)b * Hkv + kv;
-  const float* lg = logits + row * pairs * (size_t)cap + t;
   f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-  constexpr int kAt = 6;  // loads on the way (one at a time: 9.1 us of 4 x 20,000 positions, 18 pairs)
-  for (int i0 = 0; i0 < pairs; i0 += kAt) {
-    f32x4 s[kAt];
-    float z[kAt];
-#pragma unroll
-    for (int k = 0; k < kAt; ++k) {
-      const int i = min(i0 + k, pairs - 1);
-      s[k] = *reinterpret_cast<const f32x4*>(lg + (size_t)i * cap);
-      z[k] = i0 + k < pairs ? lse[row * pairs + i] : INFINITY;
-    }
-#pragma unroll
-    for (int k = 0; k < kAt; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += exp2_(s[k][e] - z[k]);
-  }
-  float* w = weights + row * stride + t;
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (t + e < L) w[e] += sum[e];
+  add_pairs(sum, logits + row * pairs * (size_t)cap + t, cap, lse + row * pairs, pairs);
+  store_sums(weights + row * stride, t, L, sum);
 }
 
 template <int D, bool BF16, bool SUMS, int CS>
@@ -640,17 +689,19 @@ hipError_t launch_cs(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const v
                      reinterpret_cast<float*>(base + at.records), lse, logits,
                      static_cast<uint16_t*>(out), Hq, sq, Hkv, L.page_size, shift, L.num_pages,
                      max_pages, max_splits, split_cap, n_hchunks, apart, scale * 1.44269504088896340736f);
-  hipError_t e = hipGetLastError();
-  const int cap = max_pages * L.page_size;
-  if (e == hipSuccess && apart && split_cap > 1) {
-    hipLaunchKernelGGL((kv8_join_kernel<D, BF16, SUMS, CS>), dim3(pairs, Hkv, B), dim3(kThreads),
-                       D / 4 * parts * kPartBytes, stream, reinterpret_cast<const float*>(base + at.records), lens, lse,
-                       static_cast<uint16_t*>(out), Hq, sq, cap, max_splits, split_cap);
-    e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int cap = max_pages * L.page_size, sums = (cap + 4 * kThreads - 1) / (4 * kThreads);
+  if (apart && split_cap > 1) {
+    hipLaunchKernelGGL((kv8_join_kernel<D, BF16, SUMS, CS>), dim3(pairs + (SUMS ? sums : 0), Hkv, B),
+                       dim3(kThreads), D / 4 * parts * kPartBytes, stream,
+                       reinterpret_cast<const float*>(base + at.records), lens, lse,
+                       static_cast<uint16_t*>(out), logits, weights, stride, pairs, Hq, sq, cap,
+                       max_splits, split_cap);
+  } else if (SUMS) {
+    hipLaunchKernelGGL(kv8_sums_kernel, dim3(sums, Hkv, B), dim3(kThreads), 0, stream, logits, lse,
+                       lens, weights, stride, pairs, cap);
   }
-  if (e != hipSuccess || !SUMS) return e;
-  hipLaunchKernelGGL(kv8_sums_kernel, dim3((uint32_t)((cap + 1023) / 1024), Hkv, B), dim3(256), 0,
-                     stream, logits, lse, lens, weights, stride, pairs, cap);
   return hipGetLastError();
 }
 
