@@ -1,7 +1,7 @@
 // Decode attention over the 8-bit cache (format: jfkv_kv8.h): 1-4 causal query
 // tokens per request, split over the positions, whose partial results are joined
 // by the last block to finish or a second launch, and optionally the attention
-// weights of the call added up per position by another.
+// weights of the call added up per position by a second launch.
 //
 //   s_t = scale * q . k_t,  p_t = exp(s_t - max s),  o = sum p_t v_t / sum p_t
 //
