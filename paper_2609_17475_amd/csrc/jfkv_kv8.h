@@ -98,6 +98,17 @@ __device__ __forceinline__ float power2(int e) {
   return e < -126 ? 0.0f : __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
+// Accumulators of sum P c count in units of 2^e_ref; their factor where e_ref moves
+// from one reference to another.  What has been accumulated never moves down by
+// more than 84 (the kernels keep e_ref within that of the largest exponent they have
+// met).  Farther down only empty accumulators move, whose first block has a far
+// smaller exponent than 0, where e_ref starts (zeros: -126): their factor has to
+// stay finite, as zero times infinity is a NaN.
+__device__ __forceinline__ float reference_step(int from, int to) {
+  const int by = from - to;
+  return __builtin_ldexpf(1.0f, by < 100 ? by : 100);
+}
+
 // Codes of two scaled values: nearest even, saturated at +-448 (infinities),
 // NaN to +0, so that no code is ever a NaN.
 __device__ __forceinline__ float code_range(float x) {

@@ -304,7 +304,7 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 2 : 3) void kv8_decod
     e_top = max(e_top, hi);
     if (lo >= e_ref && hi <= e_ref + kRefMax) return;
     const int e = max(max(hi - kRefMax, lo - 4), e_top - kRefFloor);
-    const float f = __builtin_ldexpf(1.0f, e_ref - e);
+    const float f = reference_step(e_ref, e);
 #pragma unroll
     for (int cs = 0; cs < CS; ++cs) rescale(cs, f);
     e_ref = e;

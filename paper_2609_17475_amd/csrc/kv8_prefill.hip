@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
       // one reference for the tile's values
       if (lo < e_ref || hi > e_ref + kRefMax) {
         const int e = max(hi - kRefMax, lo - 4);
-        rescale(__builtin_ldexpf(1.0f, e_ref - e));
+        rescale(reference_step(e_ref, e));
         e_ref = e;
       }
 #pragma unroll
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
     } else {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        rescale(__builtin_ldexpf(1.0f, e_ref - split_e[t]));
+        rescale(reference_step(e_ref, split_e[t]));
         e_ref = split_e[t];
         u32x4 b[NC];
 #pragma unroll
