@@ -33,6 +33,7 @@ constexpr int kFar = 4;          // tiles by which lines are touched ahead of th
 constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
 constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
 constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
+constexpr uint32_t kZeroExp = 1;  // the exponent byte of a block of zeros
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // Column sets of 16 per wave: two share every operand of K and V; at head_dim
@@ -129,6 +130,13 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
     if (at.slot == P) at.slot = 0, ++at.page;
   };
   auto page_of = [&](const Place& at) JF_INLINE { return table[min(at.page, last_page)]; };
+  // A tile without a page in the pool travels as page 0's, but counts as a tile of
+  // zeros that nobody sees: page 0's codes may be NaN and its exponents are someone
+  // else's.  (Its values are cleared by a mask on every tile.  Times against none at
+  // all, 2,048 rows over 65,536 positions and, d = 256, 256 over 196,608: 0.96 and
+  // 0.99; with a branch around the mask 1.00 and 1.02, around the products instead
+  // 1.01 and 1.00.)
+  auto held = [&](int pid) JF_INLINE { return (uint32_t)pid < (uint32_t)num_pages; };
   auto run_of = [&](int pid) JF_INLINE { return (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv; };
   const uint32_t k_off = (tid / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
   auto fetch_k = [&](int slot0, int pid) JF_INLINE {
@@ -160,11 +168,12 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
       to[0] = widen8<BF16>(k_stage[k].x, k_stage[k].y), to[64] = widen8<BF16>(k_stage[k].z, k_stage[k].w);
     }
   };
-  auto deposit_v = [&](int j) JF_INLINE {
+  auto deposit_v = [&](int j, uint32_t keep) JF_INLINE {  // keep: all ones, or 0 without a page
     if (kOf < kThreads && tid >= kOf) return;
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
       const int i = tid + k * kThreads;
+      v_stage[k] &= keep;
       if ((j + 1) * kTile > L) {  // slots not written yet: zeros (their codes may be NaN)
         const int left = min(max(L - (j * kTile + i / D * 16 + i % 64 / 16 * 4), 0), 4);
         v_stage[k] &= left ? 0xffffffffu >> (8 * (4 - left)) : 0u;
@@ -373,7 +382,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
       step(at);
     }
     fetch_k(slot[1], pid[1]);
-    exps = exps_next;
+    exps = held(pid[1]) ? exps_next : kZeroExp;
     deposit_k(j0);
     fetch_v(slot[1], pid[1]);
     fetch_k(slot[2], pid[2]);
@@ -398,7 +407,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
       uint32_t exps_1 = exps_next;
       auto transport = [&]() JF_INLINE {
         if (j < j1) {
-          deposit_v(j);
+          deposit_v(j, held(pid[1]) ? 0xffffffffu : 0u);
           fetch_v(slot[2], pid[2]);
         }
         if (j + 1 < j1) {
@@ -420,7 +429,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
         if (active && j < j1) softmax(j, (uint32_t)pid[1] < (uint32_t)num_pages);
         transport();
       }
-      exps = exps_1;
+      exps = held(pid[2]) ? exps_1 : kZeroExp;
 #pragma unroll
       for (int i = 0; i < 3; ++i) pid[i] = pid[i + 1], slot[i] = slot[i + 1];
       pid[3] = pid_n, slot[3] = at.slot;
