@@ -931,12 +931,14 @@ hipError_t launch_kv8_prefill(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool
 }
 
 namespace {
-// Windows whose queries fit into LDS, where every wave has a unit of positions to
-// walk over (d = 256, where K is not fetched ahead: two).  64 rows, 32/8 heads of
-// 128, over 262,080 positions 219 -> 173 us, 65,472 62 -> 55, 16,000 18.5 -> 17, but
-// 8,000 11 -> 18; 40 rows, 24/4 heads of 256, over 200,000 138 -> 117, but 30,000
-// 25 -> 27.  At d = 64 (100,000 positions of 16/2 heads, 128 rows: 60 both) the
-// vector work decides, which is the same.
+// Windows whose queries fit into LDS, where (nearly, 31 of 32) every wave has a unit
+// of positions to walk over; at d = 256, where K is not fetched ahead, two.  The
+// window / the kernel above, 64 rows of 32/8 heads of 128: over 12,564 positions 18.4
+// / 18.1 us, 15,964 17.1 / 18.8, 65,536 55 / 62, 262,144 173 / 219; just above one
+// unit per wave the second turn is half empty (20,064: 27.0 / 27.1 with 64 positions
+// per wave there, 21.6 with 32).  40 rows of 24/4 heads of 256: 30,040 27.6 / 25.5,
+// 64,040 43.8 / 48.0, 200,040 117 / 138.  At d = 64 the vector
+// work decides, which is the same (no window: there 32 positions per wave).
 template <int D>
 bool window_takes(const jf_kv_layout& L, int32_t T, int32_t Hq, int64_t keys) {
   const int64_t units = keys / (16 * kWinNS) * L.num_kv_heads;
@@ -989,20 +991,25 @@ hipError_t launch_kv8_weights(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool
   auto go = [&](auto fn) {
     return fn(L, pool, q, lse, T, Hq, block_table, prefix_len, softmax_scale, weights, stride, stream);
   };
-  // Few columns over many positions: 64 positions per wave, for fewer starts; else
-  // 32, for an even chip.  64 rows, 32/8 heads of 128, 65,472 positions 57 us
-  // against 72, 24/4 heads of 256, 30,000 34 against 44; but 8,000 positions 14.3
-  // against 12.7, and 2,048 rows without a prefix 188 against 134.  (Measured before
-  // windows had a kernel of their own.)
+  // What no window takes, 32 / 64 positions per wave: 64 where few columns meet many
+  // positions, for fewer starts, else 32, for an even chip.  800 columns of 32/8
+  // heads of 128 over 13,200 positions 40.7 / 36.0 us, 1,024 over 100,256 250 / 238;
+  // 126 of 24/4 heads of 256 over 30,021 20.3 / 18.3, 600 over 60,100 93.7 / 84.9;
+  // but 100 of 8/8 heads of 128 over 14,100 12.5 / 13.3, and 2,048 rows without a
+  // prefix 134 / 188.  At d = 64, with few products between a wave's exponentials,
+  // 32 everywhere: 512 columns of 16/2 heads over 100,064 positions 30.7 / 38.4, 896
+  // of 28/4 over 30,128 28.4 / 32.1, one of 4/4 over 100,001 16.3 / 23.9.
   const int64_t keys = (int64_t)prefix_len + T;
   const bool four = (int64_t)T * (Hq / L.num_kv_heads) <= 1024 &&
                     keys / 256 * L.num_kv_heads >= num_cus() * 3 / 2;
 #define JF_CASE(D_)                                                                          \
   if (L.head_dim == D_) {                                                                    \
-    if constexpr (D_ > 64)                                                                   \
+    if constexpr (D_ > 64) {                                                                 \
       if (window_takes<D_>(L, T, Hq, keys))                                                  \
         return bf16 ? go(launch_window_t<D_, true>) : go(launch_window_t<D_, false>);        \
-    if (four) return bf16 ? go(launch_weights_t<D_, true, 4>) : go(launch_weights_t<D_, false, 4>); \
+      if (four)                                                                              \
+        return bf16 ? go(launch_weights_t<D_, true, 4>) : go(launch_weights_t<D_, false, 4>); \
+    }                                                                                        \
     return bf16 ? go(launch_weights_t<D_, true, 2>) : go(launch_weights_t<D_, false, 2>);    \
   }
   JF_CASE(64)
