@@ -600,9 +600,15 @@ jf_status jf_tq4_reconstruct(const jf_kv_layout* layout, const void* k_words,
  *
  * Types: k_new, v_new, q and out are fp16 (JF_F16) or bf16 (JF_BF16), one type
  * per call; products run on the matrix cores with fp32 accumulation, codes
- * enter them exactly, softmax statistics and sums are fp32.  q must be finite, and
- * softmax_scale * q . k below 2^126 in magnitude.  Outputs must overlap neither
- * inputs nor workspaces.  Every function
+ * enter them exactly, softmax statistics and sums are fp32.  Beside the values
+ * (decode and chunk attention) a probability is rounded to fp16: by up to 2^-11 of
+ * itself, or 2^-25 of its row's largest where that is more.  The sum that divides
+ * them, lse and added weights are formed before that rounding.
+ * Limits of the attention calls, in magnitude: q finite, with a sum over a head's dims
+ * below 2^90; softmax_scale * k below 2^110 and softmax_scale * q . k below 2^126;
+ * v below 2^90.  (fp16 rows and an ordinary scale are far from them.)  Next to values
+ * of its head that are 2^80 times as large, a value may count as 0.
+ * Outputs must overlap neither inputs nor workspaces.  Every function
  * returns JF_ERR_UNSUPPORTED for a geometry, type or size that is not
  * implemented and JF_ERR_INVALID for NULL or misaligned pointers, bad sizes, a
  * short workspace or a scale that is not finite or not below 2^126 in magnitude;
