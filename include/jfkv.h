@@ -683,6 +683,11 @@ jf_status jf_kv8_decode_attn(const jf_kv_layout* layout,
  *              few rows share its keys among more blocks.  Its contents do not
  *              matter.  Calls that may overlap in time must not share one.
  *              Results with and without it are the same up to the order of sums.
+ *              The bytes belong to one T and prefix_len and do not grow with them
+ *              (64 rows, 32/8 heads of 128: 34.6 MB after 30,000 positions, 33.5
+ *              after 65,536; 2,048 rows after as many: none).  One workspace for many
+ *              calls has the largest of their sizes; a call that needs more than
+ *              there is can be given NULL, and is refused with less.
  * Positions on a page ID outside [0, num_pages) do not contribute. */
 jf_status jf_kv8_prefill_workspace_bytes(const jf_kv_layout* layout, int32_t T,
                                          int32_t num_q_heads, int32_t prefix_len,

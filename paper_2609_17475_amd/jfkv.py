@@ -977,6 +977,7 @@ def jf_kv8_decode_attn(pool: KV8Pool, q, block_tables, seq_lens, softmax_scale: 
 
 
 def jf_kv8_prefill_workspace_bytes(lay: Layout, T: int, num_q_heads: int, prefix_len: int) -> int:
+    """Of a call of this T and prefix_len; others, shorter ones too, can need more."""
     return _size(lib.jf_kv8_prefill_workspace_bytes, ctypes.byref(lay), T, num_q_heads, prefix_len)
 
 
@@ -1000,9 +1001,10 @@ def bind_kv8_prefill(pool: KV8Pool, q, block_table, prefix_len: int, softmax_sca
 def jf_kv8_prefill_attn(pool: KV8Pool, q, block_table, prefix_len: int, softmax_scale: float, out,
                         lse=None, workspace=None, stream=None):
     """Rows q, out [T][Hq][d] at positions prefix_len .. prefix_len + T - 1, which
-    are in the cache already, attend causally to it; lse fp32 [T][Hq].  workspace:
-    jf_kv8_prefill_workspace_bytes() bytes; without it the keys of a chunk of few
-    rows are not shared among more blocks."""
+    are in the cache already, attend causally to it; lse fp32 [T][Hq].  workspace: at
+    least jf_kv8_prefill_workspace_bytes() bytes (for many calls the largest of
+    theirs); without it the keys of a chunk of few rows are not shared among more
+    blocks."""
     bind_kv8_prefill(pool, q, block_table, prefix_len, softmax_scale, out, lse, workspace, stream)()
 
 
