@@ -736,7 +736,9 @@ jf_status jf_kv8_attn_weights(const jf_kv_layout* layout,
  *                 its contents do not matter.  Calls that may overlap in time
  *                 must not share one.
  *   kept          int32 [B][Hkv][keep]: the positions that stay, ascending, then -1
- *   kept_weights  fp32 [B][Hkv][keep]: their weights, then 0
+ *   kept_weights  fp32 [B][Hkv][keep]: their weights, then 0.  Calls that go on adding
+ *                 to them take rows of at least the new tables' capacity: copy them
+ *                 to the start of such rows, zeros behind.
  * Slots behind position m - 1 are left as they are. */
 jf_status jf_kv8_evict_workspace_bytes(const jf_kv_layout* layout, int32_t B,
                                        int32_t max_pages, int32_t keep,

@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
   uint8_t* const exps = is_v ? v_exps : k_exps;
   uint8_t* const to = codes + (run * P + j0 % P) * D;
 
-  if (tid < block) {  // (there are at least four threads per token)
+  if (tid < block) {  // (a thread per token at least: the launch has min(block * D / 16, 256), block <= 128)
     int src = -1, slot = 0;
     if (tid < live) {
       const int pos = kept[((size_t)b * Hkv + h) * keep + j0 + tid];

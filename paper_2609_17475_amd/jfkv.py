@@ -1062,6 +1062,8 @@ def jf_kv8_evict(pool: KV8Pool, block_tables, seq_lens, weights, keep: int, rece
                  workspace, kept, kept_weights, stream=None):
     """Moves, for each request and KV head, the last `recent` positions and those
     of the largest weights, min(length, keep) in all, in order into the pages of
-    dst_tables; kept int32 and kept_weights fp32 [B][Hkv][keep] say which."""
+    dst_tables; kept int32 and kept_weights fp32 [B][Hkv][keep] say which.  To go on
+    adding weights, copy kept_weights to the start of rows as long as the new tables'
+    capacity, zeros behind."""
     bind_kv8_evict(pool, block_tables, seq_lens, weights, keep, recent, dst_tables, workspace, kept,
                    kept_weights, stream)()
