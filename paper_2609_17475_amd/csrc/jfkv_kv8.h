@@ -98,6 +98,24 @@ __device__ __forceinline__ float power2(int e) {
   return e < -126 ? 0.0f : __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
+// The online softmax over blocks of exponents, in the decode and in the chunk
+// attention alike (their files say how it goes).
+constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
+constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
+constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The maximum (sum) over the four lanes that hold a column.
+__device__ __forceinline__ float col_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float col_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
 // Accumulators of sum P c count in units of 2^e_ref; their factor where e_ref moves
 // from one reference to another.  What has been accumulated never moves down by
 // more than 84 (the kernels keep e_ref within that of the largest exponent they have

@@ -43,9 +43,6 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kRow = 32;       // positions a wave takes at a time (in one page)
 constexpr int kCols = 16;      // (token, head) pairs of a block
 constexpr int kXcds = 8;
-constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
-constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
-constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
 
 // Splits of a request of L positions.  Rows per wave below which it is not cut
 // further: every split costs a start, a merge and a record.  24/4 heads, d = 256,
@@ -53,7 +50,7 @@ constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below
 // 42), 16 x 4,097 46 / 37 / 39, one request of 4,097 13.9 / 15.3 / 16.5.  32/8
 // heads, d = 128, 2 / 3 / 4 rows: 32 x 4,097 72 / 66 / 72, 8 x 9,000 37 / 36 / 37,
 // one of 4,097 9.2 / 10.1 / 10.8.
-template <int D, int CS>
+template <int D>
 __device__ __forceinline__ int splits_of(int L, int split_cap) {
   constexpr int kMinRows = D > 128 ? 5 : 3;
   const int rows = (L + kRow - 1) / kRow;
@@ -66,19 +63,8 @@ struct Row {
   uint32_t exps;  // lanes 0, 1: K's exponent bytes of the two tiles; 2, 3: V's
 };
 
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int lane_value(uint32_t x, int l) {
   return __builtin_amdgcn_readlane((int)x, l);
-}
-
-// The maximum (sum) over the four lanes that hold a column.
-__device__ __forceinline__ float col_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float col_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
 }
 
 // Partial results of some splits: sums of p v and p in units of 2^m.
@@ -164,7 +150,7 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 2 : 3) void kv8_decod
   const int c0 = hc * kCols * CS, ncols = min(kCols * CS, pairs - c0);
 
   const int L = min(max(seq_lens[b], 0), max_pages * P);
-  const int rows = (L + kRow - 1) / kRow, S = splits_of<D, CS>(L, split_cap);
+  const int rows = (L + kRow - 1) / kRow, S = splits_of<D>(L, split_cap);
   if (split >= S) return;
   const int base = rows / S, rem = rows % S;
   const int r0 = split * base + min(split, rem), r1 = r0 + base + (split < rem ? 1 : 0);
@@ -384,43 +370,31 @@ __global__ __launch_bounds__(kThreads, D > 128 || CS > 1 ? 2 : 3) void kv8_decod
   };
 
   if (r0 < r1) {
-    // NB rows in flight.  One is enough: four waves then keep 32 KB (at d = 128) on
-    // the way per CU, and three blocks fit on one; two took 86.9 against 85.2 us at
-    // 262,144 positions and 80 against 70 for eight requests of 20,000.
-    constexpr int NB = 1;
-    Row<D> w[NB];
-    int pid[NB], ahead[NB];
+    // One row in flight: four waves then keep 32 KB (at d = 128) on the way per CU,
+    // and three blocks fit on one; two took 86.9 against 85.2 us at 262,144 positions
+    // and 80 against 70 for eight requests of 20,000.
+    Row<D> w;
+    int r = r0 + wave;
+    int pid = page_of(r), ahead = page_of(r + kWaves);
+    fetch_k(w, r, pid);
+    fetch_v(w, r, pid);
+    for (; r < r1; r += kWaves) {
+      const bool on = (uint32_t)pid < (uint32_t)num_pages;
+      float s[CS][2][4];
+      int ev[2];
+      scores(w, r, s, ev);
+      if (!on) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int r = r0 + wave + i * kWaves;
-      pid[i] = page_of(r);
-      ahead[i] = page_of(r + NB * kWaves);
-      fetch_k(w[i], r, pid[i]);
-      fetch_v(w[i], r, pid[i]);
-    }
-    for (int rr = r0 + wave; rr < r1; rr += NB * kWaves) {
+        for (int cs = 0; cs < CS; ++cs)
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int r = rr + i * kWaves, rn = r + NB * kWaves;
-        const bool on = (uint32_t)pid[i] < (uint32_t)num_pages;
-        float s[CS][2][4];
-        int ev[2];
-        if (r < r1) {
-          scores(w[i], r, s, ev);
-          if (!on) {
-#pragma unroll
-            for (int cs = 0; cs < CS; ++cs)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) s[cs][e / 4][e % 4] = -INFINITY;
-          }
-          if (SUMS) keep_scores(r, s);
-        }
-        fetch_k(w[i], rn, ahead[i]);
-        if (r < r1 && on) attend(w[i], r, s, ev);
-        fetch_v(w[i], rn, ahead[i]);
-        pid[i] = ahead[i];
-        ahead[i] = page_of(rn + NB * kWaves);
+          for (int e = 0; e < 8; ++e) s[cs][e / 4][e % 4] = -INFINITY;
       }
+      if (SUMS) keep_scores(r, s);
+      fetch_k(w, r + kWaves, ahead);
+      if (on) attend(w, r, s, ev);
+      fetch_v(w, r + kWaves, ahead);
+      pid = ahead;
+      ahead = page_of(r + 2 * kWaves);
     }
   }
 
@@ -558,7 +532,7 @@ __device__ __forceinline__ void store_sums(float* w, int64_t t, int L, const f32
 // KV head, pair).  SUMS: and workgroups behind them for the weights' sums, 1,024
 // positions each, which take the log-sum-exps from the records themselves rather
 // than wait for another launch.
-template <int D, bool BF16, bool SUMS, int CS>
+template <int D, bool BF16, bool SUMS>
 __global__ __launch_bounds__(kThreads) void kv8_join_kernel(
     const float* __restrict__ recs, const int32_t* __restrict__ seq_lens,
     const float* __restrict__ lse, uint16_t* __restrict__ out, const float* __restrict__ logits,
@@ -567,7 +541,7 @@ __global__ __launch_bounds__(kThreads) void kv8_join_kernel(
   constexpr int kPer = D / 4;
   extern __shared__ __align__(16) float smem[];
   const int pair = blockIdx.x, kv = blockIdx.y, b = blockIdx.z, Hkv = gridDim.y;
-  const int L = min(max(seq_lens[b], 0), cap), S = splits_of<D, CS>(L, split_cap);
+  const int L = min(max(seq_lens[b], 0), cap), S = splits_of<D>(L, split_cap);
   const int tid = threadIdx.x, parts = (S + kAt - 1) / kAt;
   const size_t row = (size_t)b * Hkv + kv;
   const Parts at = parts_at(smem, kPer * parts);
@@ -693,7 +667,7 @@ hipError_t launch_cs(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, const v
   if (e != hipSuccess) return e;
   const int cap = max_pages * L.page_size, sums = (cap + 4 * kThreads - 1) / (4 * kThreads);
   if (apart && split_cap > 1) {
-    hipLaunchKernelGGL((kv8_join_kernel<D, BF16, SUMS, CS>), dim3(pairs + (SUMS ? sums : 0), Hkv, B),
+    hipLaunchKernelGGL((kv8_join_kernel<D, BF16, SUMS>), dim3(pairs + (SUMS ? sums : 0), Hkv, B),
                        dim3(kThreads), D / 4 * parts * kPartBytes, stream,
                        reinterpret_cast<const float*>(base + at.records), lens, lse,
                        static_cast<uint16_t*>(out), logits, weights, stride, pairs, Hq, sq, cap,

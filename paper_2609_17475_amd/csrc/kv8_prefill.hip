@@ -30,9 +30,6 @@ constexpr int kTile = 64;        // positions of a tile (in one page)
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kFar = 4;          // tiles by which lines are touched ahead of their fetch
-constexpr float kMargin = 4.0f;  // m is raised where a score exceeds it by more (log2)
-constexpr int kRefMax = 10;      // e_v - e_ref stays in 0 .. kRefMax
-constexpr int kRefFloor = 80;    // e_ref is not lowered further than this below the largest e_v
 constexpr uint32_t kZeroExp = 1;  // the exponent byte of a block of zeros
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -45,16 +42,6 @@ constexpr int col_sets() {
 template <int D>
 constexpr int block_cols() {
   return kWaves * 16 * col_sets<D>();
-}
-
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float col_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float col_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
 }
 
 // The query row of (row, head) as B operands: dims 64 c + 16 g + 8 j ..
@@ -97,8 +84,7 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
   // the wave's columns
   const int64_t wcol = col_base + wave * 16 * NC;
   const bool active = wcol < ncols;
-  const int w_lo = active ? (int)(wcol / gq) : 0;  // its first and last row
-  const int w_hi = active ? (int)((min(wcol + 16 * NC, ncols) - 1) / gq) : -1;
+  const int w_lo = active ? (int)(wcol / gq) : 0;  // its first row
   int row[NC];
   u32x4 qf[NC][C][2];
 #pragma unroll
@@ -664,7 +650,8 @@ __global__ __launch_bounds__(kWThreads, NS > 2 ? 2 : 3) void kv8_weights_kernel(
   }
   if (!on) return;
   // Sums over the 16 lanes that share the positions: halved turn by turn, until
-  // lane n holds the sum of position 16 (n / 4) + 4 g + n % 4.
+  // lane n holds the sum of position 16 (n / 4) + 4 g + n % 4.  (Written out in both
+  // kernels: as a function of w it takes registers, and at d = 256 spills, more.)
   float v[4 * NS];
 #pragma unroll
   for (int i = 0; i < 4 * NS; ++i) v[i] = w[i / 4][i % 4];
