@@ -5,11 +5,13 @@
 //   s_it = scale * q_i . k_t  (t <= prefix + i),  lse_i = log sum_t exp(s_it)
 //   o_i = sum_t exp(s_it - lse_i) v_t,  w_t += sum_i exp(s_it - lse_i)
 //
-// Bound by the matrix cores and the vector work beside them (an exponential and
-// three more instructions per score): a SIMD's vector instructions take ~4.7
-// cycles each and every matrix product holds up another 6-8.  The
-// (row, head) pairs that read a KV head are the columns of the products, as in
-// kv8_decode.hip, whose operand layouts and exponents' handling are the same.
+// Bound by the vector work beside the matrix cores, an exponential and some four
+// instructions per score: at d = 128 vector instructions issue in 54 % of a SIMD's
+// cycles and its matrix core is busy in 39 %, and the two hardly overlap.  The (row,
+// head) pairs that read a KV head are the columns of the products, as in
+// kv8_decode.hip, whose operand layouts, exponents' handling and roundings (P to fp16
+// beside the values) are the same.  2,048 rows of 32/8 heads of 128 over 65,536
+// positions take 2.33 ms (0.96 PFLOP/s), 256 of 24/4 heads of 256 over 196,608 1.35.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -355,8 +357,8 @@ __global__ __launch_bounds__(kThreads) void kv8_prefill_kernel(
   // the vector work (the softmax, the next tiles' way into LDS) after them, the
   // second the other way round, so that one's matrix products meet the other's
   // vector work (d = 256: 256 rows over 196,608 positions 1,790 -> 1,430 us; at d =
-  // 64, where the vector work is the most, all do the same).  (Two loops, as one loop with both orders spills; every wave
-  // passes j1 - j0 + 1 barriers in either.)
+  // 64, where the vector work is the most, all do the same).  (Two loops, as one loop
+  // with both orders spills; every wave passes j1 - j0 + 1 barriers in either.)
   auto walk = [&](auto is_late) JF_INLINE {
     constexpr bool late = decltype(is_late)::value;
     Place at = {j0 * kTile / P, j0 * kTile % P};
@@ -883,7 +885,11 @@ int shift_of(int block) {
 // Splits of a chunk's tiles: the count with the least estimated time.  A turn
 // of the chip takes the tiles of its longest block and a start and end worth
 // about four; the partials are written and read once, at about 4 TB/s, and
-// joined by a second launch (a tile takes about 1.7 us).
+// joined by a second launch, at a tile's 1.7 us.  (That is what a tile takes at d =
+// 64; it takes 2.1-2.2 at 128 and 256.  With these a tenth of all shapes are cut
+// differently, few of them for more than a microsecond: at d = 128 some short chunks
+// without a prefix gain, 304 rows of 8/8 heads 20.2 -> 17.9 us, others lose, 115 of
+// 16/4 over 1,255 23.6 -> 24.4.)
 int kv8_prefill_splits(const jf_kv_layout& L, int32_t T, int32_t Hq, int32_t prefix) {
   const int cols = L.head_dim == 256 ? block_cols<256>() : L.head_dim == 128 ? block_cols<128>() : block_cols<64>();
   const int64_t ncols = (int64_t)T * (Hq / L.num_kv_heads);
