@@ -379,6 +379,9 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
   __syncthreads();
   for (int v = 0; v < (nthr >> 6); ++v) top = max(top, s_max[v]);
 
+  // The factor of a token's codes.  Where one is not 0 it is at most 2^17; bounded
+  // for the zeros of blocks with larger exponents, as infinity would make them NaN.
+  auto factor = [&](int t) { return __builtin_ldexpf(1.0f, min(s_exp[t] - top, 100)); };
 #pragma unroll
   for (int k = 0; k < NI; ++k) {
     const int i = tid + k * nthr;
@@ -386,7 +389,7 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
     if (!is_v) {
       const int t = i >> (dl - 4);
       if (t >= live) continue;
-      const float f = __builtin_ldexpf(1.0f, s_exp[t] - top);
+      const float f = factor(t);
       *dst = make_uint4(rescale4(raw[k][0], f), rescale4(raw[k][1], f), rescale4(raw[k][2], f),
                         rescale4(raw[k][3], f));
     } else {
@@ -395,7 +398,7 @@ __global__ __launch_bounds__(256) void kv8_move_kernel(
       uint32_t c[4], o[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        c[j] = rescale4(raw[k][j], __builtin_ldexpf(1.0f, s_exp[t0 + j] - top));
+        c[j] = rescale4(raw[k][j], factor(t0 + j));
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt)
         o[dt] = ((c[0] >> 8 * dt) & 255u) | ((c[1] >> 8 * dt) & 255u) << 8 |
