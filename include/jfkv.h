@@ -751,6 +751,104 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
                        void* workspace, size_t workspace_bytes, int32_t* kept,
                        float* kept_weights, hipStream_t stream);
 
+/* ---------------------------------------------------- rotary positions
+ * Rows of queries and keys rotated by their tokens' positions, as the models whose
+ * caches this library keeps do before attention.  Of a head's dims the first rot_dim
+ * are rotated in rot_dim / 2 pairs, pair i of a token at position p by the angle
+ * p * f_i; the others stay:
+ *   (y1, y2) = (x1 c - x2 s, x2 c + x1 s),  c = m cos(p f_i),  s = m sin(p f_i)
+ * A pair is dims i and i + rot_dim / 2 (JF_ROPE_HALVES) or 2 i and 2 i + 1
+ * (JF_ROPE_PAIRS).  c and s are fp32 values of a table that a step forms once for all
+ * of its layers (and a training program once); each product and sum is rounded in
+ * fp32, the result once to the rows' type (JF_F16 or JF_BF16). */
+typedef enum { JF_ROPE_HALVES = 0, JF_ROPE_PAIRS = 1 } jf_rope_order;
+
+/* How frequencies f_i = base^(-2 i / rot_dim) are changed for contexts `factor` times
+ * as long as the model's own (original_len positions):
+ *   JF_ROPE_PLAIN    not at all
+ *   JF_ROPE_LINEAR   f_i / factor (position interpolation)
+ *   JF_ROPE_BASE     base * factor^(rot_dim / (rot_dim - 2)) in base's place: the
+ *                    fastest pair stays, the slowest is divided by factor
+ *   JF_ROPE_PARTS    pairs of more than `fast` turns in original_len positions stay,
+ *                    those of fewer than `slow` are divided by factor, between them
+ *                    lies a ramp over the pairs' numbers ("YaRN", arXiv 2309.00071):
+ *                    i(r) = rot_dim ln(original_len / (2 pi r)) / (2 ln base), the ramp
+ *                    from floor(i(fast)), at least 0, to ceil(i(slow)), at most
+ *                    rot_dim - 1; m = 0.1 ln(factor) + 1 (factor <= 1: 1) */
+typedef enum {
+  JF_ROPE_PLAIN = 0,
+  JF_ROPE_LINEAR = 1,
+  JF_ROPE_BASE = 2,
+  JF_ROPE_PARTS = 3
+} jf_rope_scaling;
+
+/* The frequencies and the magnitude m (1 but for JF_ROPE_PARTS), on the host.  Formed
+ * in 64 bits, rounded once to fp32.  inv_freq: float [rot_dim / 2] (host);
+ * magnitude: float (host).  base > 1; factor > 0 (unless PLAIN); for PARTS
+ * original_len >= 1 and fast > slow > 0.  Arguments a scaling does not use are not
+ * looked at.  rot_dim even, 2 .. 65536 (BASE: from 4 on). */
+jf_status jf_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor,
+                              int32_t original_len, double fast, double slow, float* inv_freq,
+                              float* magnitude);
+
+/* table[j][i] = (c, s) of position positions[j] and frequency inv_freq[i]:
+ *   positions  int32 [n] (device), any values
+ *   inv_freq   fp32 [rot_dim / 2] (device), magnitudes that keep |p f| below 2^40
+ *   table      fp32 [n][rot_dim / 2][2] (device, 8-byte aligned)
+ * The angle is exact (64 bits and a rest), c and s are rounded once to fp32. */
+jf_status jf_rope_table(const int32_t* positions, int32_t n, const float* inv_freq,
+                        int32_t rot_dim, float magnitude, float* table, hipStream_t stream);
+
+/* The angles of a call's tokens: token j takes row rows[j] of the table (int32
+ * [total_tok], device; an entry outside the table is cut to its first or last row), or
+ * row j where rows is NULL (the table then has at least total_tok rows). */
+typedef struct {
+  const float* table;  /* [table_rows][rot_dim / 2][2], device, 8-byte aligned */
+  const int32_t* rows;
+  int32_t table_rows;
+  int32_t rot_dim;     /* even */
+  int32_t order;       /* jf_rope_order */
+} jf_rope;
+
+/* Rotate rows of queries and of keys in one launch; transpose != 0: s with the other
+ * sign, which turns back (m = 1) and takes gradients of the outputs to gradients of
+ * the inputs.
+ *   q, k   [total_tok][heads][head_dim] (device), a token's heads one after the other,
+ *          q_stride (k_stride) elements from one token to the next: rows of their own,
+ *          or part of a wider projection's rows.  num_q_heads = 0 or num_k_heads = 0:
+ *          none (the pointers are not looked at).
+ *   q_out, k_out   the same shape and strides of their own.  An output may be its
+ *          input (same pointer and stride); otherwise the memory of outputs must not
+ *          overlap that of inputs or of the other output.
+ * head_dim even and at most 65536, rot_dim <= head_dim, strides at least heads *
+ * head_dim where total_tok > 1.  Addresses aligned to an element are enough; 16 bytes,
+ * with sizes and strides of multiples of 16 and 8 elements, are fastest. */
+jf_status jf_rope_rotate(const jf_rope* rope, int32_t dtype, int32_t head_dim, int32_t transpose,
+                         const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                         int32_t num_q_heads, const void* k, int64_t k_stride, void* k_out,
+                         int64_t k_out_stride, int32_t num_k_heads, int32_t total_tok,
+                         hipStream_t stream);
+
+/* jf_kv8_append of keys that are rotated on the way, and the rotation of the same
+ * tokens' queries, in one launch: the cache and q_out are, bit for bit, those of
+ * jf_rope_rotate followed by jf_kv8_append.
+ *   rope      as above, rot_dim a multiple of 16 and at most the layout's head_dim
+ *   k_new, v_new  [total_tok][Hkv][d] (device, 16-byte aligned), k_stride and
+ *             v_stride elements from one token to the next (multiples of 8, at least
+ *             Hkv * d where total_tok > 1)
+ *   q, q_out  NULL, or [total_tok][num_q_heads][d] (device, 16-byte aligned), q with
+ *             q_stride as above, q_out without gaps; q_out may be q where q has none
+ * The positions that turn a key need not be the cache's (after an eviction they are
+ * not).  Other arguments and rules as jf_kv8_append; every token's query is rotated,
+ * also those whose keys are skipped. */
+jf_status jf_kv8_rope_append(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
+                             int32_t dtype, const jf_rope* rope, const void* k_new,
+                             int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
+                             int64_t q_stride, void* q_out, int32_t num_q_heads,
+                             const int32_t* cu_tok, const int32_t* start_pos,
+                             const int32_t* block_tables, int32_t B, int32_t max_pages,
+                             int32_t total_tok, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

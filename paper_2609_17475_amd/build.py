@@ -21,7 +21,7 @@ ARCH = os.environ.get("JFKV_ARCH", "gfx950")
 
 SOURCES = ["jfkv_host.cpp", "quantize.hip", "decode.hip", "prefill.hip", "tq4.hip",
            "tq4_decode.hip", "reconstruct.hip", "pages.hip", "calib.hip", "kv8_host.cpp",
-           "kv8_append.hip", "kv8_decode.hip", "kv8_prefill.hip", "kv8_evict.hip"]
+           "kv8_append.hip", "kv8_decode.hip", "kv8_prefill.hip", "kv8_evict.hip", "rope_host.cpp", "rope.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]

@@ -121,6 +121,27 @@ hipError_t launch_kv8_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
                              const int32_t* start_pos, const int32_t* block_tables, int32_t B,
                              int32_t max_pages, int32_t total_tok, hipStream_t stream);
 
+// Rotary positions (rope.hip).  Rows of `heads` heads for each token, `stride`
+// elements apart.
+struct RopeRows {
+  const void* from = nullptr;
+  void* to = nullptr;
+  int64_t from_stride = 0, to_stride = 0;
+  int32_t heads = 0;
+};
+hipError_t launch_rope_table(const int32_t* positions, int32_t n, const float* inv_freq, int32_t rot,
+                             float magnitude, float* table, hipStream_t stream);
+hipError_t launch_rope_rotate(const jf_rope& rope, bool bf16, bool transpose, int32_t head_dim,
+                              const RopeRows& q, const RopeRows& k, int32_t total_tok,
+                              hipStream_t stream);
+// The append with k rotated on the way, and rows of queries (q may be nullptr).
+hipError_t launch_kv8_rope_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                                  const jf_rope& rope, const void* k_new, int64_t k_stride,
+                                  const void* v_new, int64_t v_stride, const void* q,
+                                  int64_t q_stride, void* q_out, int32_t Hq, const int32_t* cu_tok,
+                                  const int32_t* start_pos, const int32_t* block_tables, int32_t B,
+                                  int32_t max_pages, int32_t total_tok, hipStream_t stream);
+
 // Decode workspace: the completion counters and split records of the decode
 // over 4-bit pages (Hq * sq heads); where weights are added up, then the
 // log-sum-exps [B][Hkv][pairs] and the scores [B][Hkv][pairs][cap] of the call

@@ -19,8 +19,11 @@
 
 #include <algorithm>
 
+#include <type_traits>
+
 #include "jfkv_internal.h"
 #include "jfkv_kv8.h"
+#include "jfkv_rope.h"
 
 namespace jfkv {
 namespace {
@@ -48,21 +51,111 @@ __device__ __forceinline__ Span span_of(const int32_t* cu, const int32_t* start,
   return {r0, (int)st, (int)n, blocks};
 }
 
+// What the call with a rotation has besides: the rows' angles, strides of their own,
+// and rows of queries.
+struct Turn {
+  const float* table;
+  const int32_t* rows;
+  int table_rows, half;
+  bool pairs;
+  int64_t k_stride, v_stride, q_stride;
+  const uint16_t* q;
+  uint16_t* q_out;
+  int q_heads;
+};
+struct NoTurn {};
+
+// 8 dims of a row of head_dim D, from dim `base` on, rotated; the partner dims are
+// read from the row as well (they are another lane's, in the first-level cache).
+template <bool BF16>
+__device__ __forceinline__ void turn8(uint32_t (&raw)[4], const uint16_t* x, const float* angles,
+                                      int base, int half, bool pairs) {
+  using namespace rope;
+  if (base >= 2 * half) return;
+  if (pairs) {
+    Angles<4> w;
+    w.load(angles, base / 8, 1.0f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float y1, y2;
+      turn2(half_to_float<BF16>(raw[k] & 0xffffu), half_to_float<BF16>(raw[k] >> 16), w.a[k], y1, y2);
+      raw[k] = narrow2<BF16>(y1, y2);
+    }
+    return;
+  }
+  const bool second = base >= half;
+  Angles<8> w;  // (the second of a pair: x2 c + x1 s = x2 c - x1 (-s))
+  w.load(angles, (second ? base - half : base) / 8, second ? -1.0f : 1.0f);
+  Elements<8> p;
+  p.load(x + (second ? base - half : base + half));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float y[2], other;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      turn2(half_to_float<BF16>(i ? raw[k] >> 16 : raw[k] & 0xffffu), p.template get<BF16>(2 * k + i),
+            w.a[2 * k + i], y[i], other);
+    raw[k] = narrow2<BF16>(y[0], y[1]);
+  }
+}
+
+// The rows of queries, a token's heads by a block at a time.
+template <bool BF16, bool PAIRS>
+__device__ __forceinline__ void turn_queries(const Turn& r, int D, int64_t block, int64_t blocks,
+                                             int total) {
+  using namespace rope;
+  const int items = D / 16, n_rot = r.half / 8;
+  for (int64_t t = block; t < total; t += blocks) {
+    const float* const angles = r.table + row_of(r.rows, r.table_rows, t) * (2 * (int64_t)r.half);
+    for (int i = threadIdx.x; i < r.q_heads * items; i += blockDim.x) {
+      const int item = i % items, at = i / items * D;
+      int first, second;
+      places<8, PAIRS>(item, n_rot, first, second);
+      const uint16_t* const x = r.q + t * r.q_stride + at;
+      uint16_t* const y = r.q_out + t * ((int64_t)r.q_heads * D) + at;
+      Elements<8> x1, x2;
+      x1.load(x + first);
+      x2.load(x + second);
+      if (item < n_rot) {
+        Angles<8> w;
+        w.load(angles, item, 1.0f);
+        turn<8, BF16, PAIRS>(x1, x2, w);
+      }
+      x1.store(y + first);
+      x2.store(y + second);
+    }
+  }
+}
+
 // NI items of 16 elements per thread: for K 16 dims of a token, for V 4 dims
-// of 4 tokens (the 16 bytes that lie together in the pool).
-template <int NI, bool BF16>
+// of 4 tokens (the 16 bytes that lie together in the pool).  ROPE: K's rows are
+// rotated on the way, rounded to their type as a rotation by itself would leave
+// them, so that both ways write the same cache; blocks of z = 2 rotate queries.
+template <int NI, bool BF16, bool ROPE>
 __global__ __launch_bounds__(256) void kv8_append_kernel(
     uint8_t* __restrict__ k_codes, uint8_t* __restrict__ k_exps, uint8_t* __restrict__ v_codes,
     uint8_t* __restrict__ v_exps, const uint16_t* __restrict__ k_new,
     const uint16_t* __restrict__ v_new, const int32_t* __restrict__ cu,
     const int32_t* __restrict__ start, const int32_t* __restrict__ block_tables, int B, int Hkv,
-    int D, int P, int block, int num_pages, int max_pages, int total) {
+    int D, int P, int block, int num_pages, int max_pages, int total,
+    std::conditional_t<ROPE, Turn, NoTurn> rope) {
   constexpr uint32_t kInf = BF16 ? 0x7f80u : 0x7c00u;  // magnitudes from here on are not finite
   __shared__ uint32_t s_max[4];
   const int tid = threadIdx.x, lane = tid & 63, nthr = blockDim.x;
   const int h = blockIdx.y;
   const bool is_v = blockIdx.z != 0;
   const int64_t cap = (int64_t)max_pages * P;
+  if constexpr (ROPE) {
+    if (blockIdx.z == 2) {
+      const int64_t units = (int64_t)gridDim.x * gridDim.y;
+      const int64_t unit = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+      if (rope.pairs)
+        turn_queries<BF16, true>(rope, D, unit, units, total);
+      else
+        turn_queries<BF16, false>(rope, D, unit, units, total);
+      return;
+    }
+  }
 
   // ---- the request and block of this unit: every wave scans the block counts
   int u = blockIdx.x, b = 0;
@@ -109,7 +202,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
 
   // element offset of slot s's row (in range for lo <= s < hi)
   const int64_t row_base = sp.r0 + pos0 - sp.st;
-  const size_t row_stride = (size_t)Hkv * D;
+  size_t row_stride = (size_t)Hkv * D;
+  if constexpr (ROPE) row_stride = is_v ? rope.v_stride : rope.k_stride;
   const uint16_t* const xh = x + (size_t)h * D;
 
   // ---- load, and the largest finite magnitude as 16-bit patterns
@@ -127,6 +221,18 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
         const uint4 a = src[0], d = src[1];
         raw[k][0] = a.x, raw[k][1] = a.y, raw[k][2] = a.z, raw[k][3] = a.w;
         raw[k][4] = d.x, raw[k][5] = d.y, raw[k][6] = d.z, raw[k][7] = d.w;
+        if constexpr (ROPE) {
+          const uint16_t* const row = xh + (row_base + t) * row_stride;
+          const float* const angles =
+              rope.table + rope::row_of(rope.rows, rope.table_rows, row_base + t) * (2 * (int64_t)rope.half);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t part[4] = {raw[k][4 * j], raw[k][4 * j + 1], raw[k][4 * j + 2], raw[k][4 * j + 3]};
+            turn8<BF16>(part, row, angles, 16 * c + 8 * j, rope.half, rope.pairs);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[k][4 * j + i] = part[i];
+          }
+        }
       }
     } else {
       const int r = i % D, t0 = (i / D) * 16 + (r % 64) / 16 * 4, dim = r / 64 * 64 + (r % 16) * 4;
@@ -214,31 +320,56 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
 
 }  // namespace
 
-hipError_t launch_kv8_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
-                             const void* k_new, const void* v_new, const int32_t* cu_tok,
-                             const int32_t* start_pos, const int32_t* block_tables, int32_t B,
-                             int32_t max_pages, int32_t total_tok, hipStream_t stream) {
+namespace {
+template <bool ROPE, class T>
+hipError_t launch_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                         const void* k_new, const void* v_new, const int32_t* cu_tok,
+                         const int32_t* start_pos, const int32_t* block_tables, int32_t B,
+                         int32_t max_pages, int32_t total_tok, const T& rope, int parts,
+                         hipStream_t stream) {
   const int block = L.group_size, items = block * L.head_dim / 16;
   const int threads = std::min(items, 256);
   // blocks that total_tok rows of B requests can touch: one per row at most,
   // and whole blocks plus two partial ones per request
   const int64_t units = std::min<int64_t>(total_tok, total_tok / block + 2 * (int64_t)B);
-  const dim3 grid((uint32_t)units, L.num_kv_heads, 2);
+  const dim3 grid((uint32_t)units, L.num_kv_heads, parts);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<uint8_t*>(pool.k_codes),
                        static_cast<uint8_t*>(pool.k_meta), static_cast<uint8_t*>(pool.v_codes),
                        static_cast<uint8_t*>(pool.v_meta), static_cast<const uint16_t*>(k_new),
                        static_cast<const uint16_t*>(v_new), cu_tok, start_pos, block_tables, B,
                        L.num_kv_heads, L.head_dim, L.page_size, block, L.num_pages, max_pages,
-                       total_tok);
+                       total_tok, rope);
     return hipGetLastError();
   };
   switch (items / threads) {
-    case 1: return bf16 ? go(kv8_append_kernel<1, true>) : go(kv8_append_kernel<1, false>);
-    case 2: return bf16 ? go(kv8_append_kernel<2, true>) : go(kv8_append_kernel<2, false>);
-    case 4: return bf16 ? go(kv8_append_kernel<4, true>) : go(kv8_append_kernel<4, false>);
-    default: return bf16 ? go(kv8_append_kernel<8, true>) : go(kv8_append_kernel<8, false>);
+    case 1: return bf16 ? go(kv8_append_kernel<1, true, ROPE>) : go(kv8_append_kernel<1, false, ROPE>);
+    case 2: return bf16 ? go(kv8_append_kernel<2, true, ROPE>) : go(kv8_append_kernel<2, false, ROPE>);
+    case 4: return bf16 ? go(kv8_append_kernel<4, true, ROPE>) : go(kv8_append_kernel<4, false, ROPE>);
+    default: return bf16 ? go(kv8_append_kernel<8, true, ROPE>) : go(kv8_append_kernel<8, false, ROPE>);
   }
+}
+}  // namespace
+
+hipError_t launch_kv8_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                             const void* k_new, const void* v_new, const int32_t* cu_tok,
+                             const int32_t* start_pos, const int32_t* block_tables, int32_t B,
+                             int32_t max_pages, int32_t total_tok, hipStream_t stream) {
+  return launch_append<false>(L, pool, bf16, k_new, v_new, cu_tok, start_pos, block_tables, B,
+                              max_pages, total_tok, NoTurn{}, 2, stream);
+}
+
+hipError_t launch_kv8_rope_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                                  const jf_rope& r, const void* k_new, int64_t k_stride,
+                                  const void* v_new, int64_t v_stride, const void* q, int64_t q_stride,
+                                  void* q_out, int32_t Hq, const int32_t* cu_tok,
+                                  const int32_t* start_pos, const int32_t* block_tables, int32_t B,
+                                  int32_t max_pages, int32_t total_tok, hipStream_t stream) {
+  const Turn turn{r.table, r.rows, r.table_rows, r.rot_dim / 2, r.order == JF_ROPE_PAIRS,
+                  k_stride, v_stride, q_stride, static_cast<const uint16_t*>(q),
+                  static_cast<uint16_t*>(q_out), Hq};
+  return launch_append<true>(L, pool, bf16, k_new, v_new, cu_tok, start_pos, block_tables, B,
+                             max_pages, total_tok, turn, q ? 3 : 2, stream);
 }
 
 }  // namespace jfkv

@@ -35,6 +35,7 @@ EXPORTS = [
     "jf_kv8_pool_bytes", "jf_kv8_append", "jf_kv8_decode_workspace_bytes", "jf_kv8_decode_attn",
     "jf_kv8_prefill_workspace_bytes", "jf_kv8_prefill_attn", "jf_kv8_attn_weights",
     "jf_kv8_evict_workspace_bytes", "jf_kv8_evict",
+    "jf_rope_frequencies", "jf_rope_table", "jf_rope_rotate", "jf_kv8_rope_append",
 ]
 
 
@@ -53,6 +54,12 @@ class Layout(ctypes.Structure):
 class PoolPtrs(ctypes.Structure):
     _fields_ = [("k_codes", ctypes.c_void_p), ("k_meta", ctypes.c_void_p),
                 ("v_codes", ctypes.c_void_p), ("v_meta", ctypes.c_void_p)]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("table_rows", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("order", ctypes.c_int32)]
 
 
 def _load():
@@ -120,6 +127,12 @@ def _load():
                                      P]),
         "jf_kv8_evict_workspace_bytes": (st, [P, i32, i32, i32, ctypes.POINTER(sz)]),
         "jf_kv8_evict": (st, [P, P, i32, P, i32, P, P, i64, i32, i32, P, i32, P, sz, P, P, P]),
+        "jf_rope_frequencies": (st, [i32, ctypes.c_double, i32, ctypes.c_double, i32,
+                                     ctypes.c_double, ctypes.c_double, P, P]),
+        "jf_rope_table": (st, [P, i32, P, i32, ctypes.c_float, P, P]),
+        "jf_rope_rotate": (st, [P, i32, i32, i32, P, i64, P, i64, i32, P, i64, P, i64, i32, i32, P]),
+        "jf_kv8_rope_append": (st, [P, P, i32, P, P, i64, P, i64, P, i64, P, i32, P, P, P, i32, i32,
+                                    i32, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -1067,3 +1080,167 @@ def jf_kv8_evict(pool: KV8Pool, block_tables, seq_lens, weights, keep: int, rece
     capacity, zeros behind."""
     bind_kv8_evict(pool, block_tables, seq_lens, weights, keep, recent, dst_tables, workspace, kept,
                    kept_weights, stream)()
+
+
+# ------------------------------------------------------- rotary positions
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "plain",
+                     factor: float = 1.0, original_len: int = 0, fast: float = 32.0,
+                     slow: float = 1.0):
+    """(fp32 CPU tensor [rot_dim / 2], magnitude) of rotary positions; `scaling` for
+    contexts `factor` times as long as the model's own: "plain", "linear", "base" or
+    "parts" (see include/jfkv.h)."""
+    import torch
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError("scaling must be one of %s" % ", ".join(ROPE_SCALINGS))
+    f, m = torch.empty(max(rot_dim // 2, 1), dtype=torch.float32), ctypes.c_float()
+    _check(lib.jf_rope_frequencies(rot_dim, base, ROPE_SCALINGS[scaling], factor, original_len,
+                                   fast, slow, f.data_ptr(), ctypes.byref(m)))
+    return f, m.value
+
+
+def _here(*tensors):
+    """All on the current device."""
+    import torch
+    for t, name in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError("%s is on %s, the current device is cuda:%d" % (
+                name, t.device, torch.cuda.current_device()))
+
+
+def bind_rope_table(positions, inv_freq, table, magnitude: float = 1.0, stream=None) -> BoundCall:
+    """jf_rope_table with its arguments checked and marshalled once."""
+    import torch
+    _dev_check(positions, "positions", torch.int32)
+    _dev_check(inv_freq, "inv_freq", torch.float32)
+    _dev_check(table, "table", torch.float32)
+    _here((positions, "positions"), (inv_freq, "inv_freq"), (table, "table"))
+    if positions.dim() != 1 or inv_freq.dim() != 1 or \
+            tuple(table.shape) != (positions.shape[0], inv_freq.shape[0], 2):
+        raise ValueError("positions must be [n], inv_freq [rot_dim / 2], table [n][rot_dim / 2][2]")
+    args = (_ptr(positions), positions.shape[0], _ptr(inv_freq), 2 * inv_freq.shape[0],
+            float(magnitude), _ptr(table), _stream(stream))
+    return BoundCall(lib.jf_rope_table, args, (positions, inv_freq, table))
+
+
+def jf_rope_table(positions, inv_freq, table, magnitude: float = 1.0, stream=None):
+    """table fp32 [n][rot_dim / 2][2]: (cos, sin) of positions int32 [n] times inv_freq
+    fp32 [rot_dim / 2], times magnitude."""
+    bind_rope_table(positions, inv_freq, table, magnitude, stream)()
+
+
+class Rope:
+    """The angles of a call's tokens: token j takes row rows[j] (int32) of `table`, or
+    row j; `pairs`: a pair's dims lie side by side instead of half the rotated dims
+    apart."""
+
+    def __init__(self, table, rows=None, pairs: bool = False):
+        import torch
+        _dev_check(table, "table", torch.float32)
+        _dev_check(rows, "rows", torch.int32)
+        if table.dim() != 3 or table.shape[2] != 2:
+            raise ValueError("table must be [rows][rot_dim / 2][2]")
+        if rows is not None and rows.dim() != 1:
+            raise ValueError("rows must be [total_tok]")
+        self.table, self.rows, self.pairs = table, rows, bool(pairs)
+
+    def args(self, tokens: int) -> RopeArgs:
+        if self.rows is not None and self.rows.shape[0] != tokens:
+            raise ValueError("rows must be [total_tok]")
+        _here((self.table, "table"), (self.rows, "rows"))
+        return RopeArgs(_ptr(self.table), _ptr(self.rows), self.table.shape[0],
+                        2 * self.table.shape[1], ROPE_PAIRS if self.pairs else ROPE_HALVES)
+
+
+def _rope_type(*tensors) -> int:
+    """JF_ type of rows (all the same), their device checked."""
+    import torch
+    given = [(t, name) for t, name in tensors if t is not None]
+    dtype = given[0][0].dtype
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("%s must be float16 or bfloat16, got %s" % (given[0][1], dtype))
+    for t, name in given:
+        if not t.is_cuda:
+            raise ValueError("%s must be a device tensor" % name)
+        if t.dtype != dtype:
+            raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    _here(*given)
+    return JF_BF16 if dtype == torch.bfloat16 else JF_F16
+
+
+def _rope_stride(t, name: str) -> int:
+    """Elements from one token of [tokens][heads][d] to the next."""
+    if t.dim() != 3:
+        raise ValueError("%s must be [total_tok][heads][head_dim]" % name)
+    n, h, d = t.shape
+    if t.numel() and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+        raise ValueError("the heads of a token of %s must lie one after the other" % name)
+    return t.stride(0) if n > 1 else h * d
+
+
+def bind_rope_rotate(rope: Rope, q, q_out, k=None, k_out=None, transpose: bool = False,
+                     stream=None) -> BoundCall:
+    """jf_rope_rotate with its arguments checked and marshalled once."""
+    dt = _rope_type((q, "q"), (q_out, "q_out"), (k, "k"), (k_out, "k_out"))
+    tail, keep = [], (rope.table, rope.rows, q, q_out, k, k_out)
+    for x, y, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if (x is None) != (y is None):
+            raise ValueError("%s and %s_out are given both or neither" % (name, name))
+        if x is None:
+            tail += [None, 0, None, 0, 0]
+            continue
+        if x.shape != y.shape:
+            raise ValueError("%s and %s_out differ in shape" % (name, name))
+        tail += [_ptr(x), _rope_stride(x, name), _ptr(y), _rope_stride(y, name + "_out"), x.shape[1]]
+    if k is not None and q is not None and (k.shape[0], k.shape[2]) != (q.shape[0], q.shape[2]):
+        raise ValueError("q and k differ in tokens or head_dim")
+    x = q if q is not None else k
+    args = rope.args(x.shape[0])
+    return BoundCall(lib.jf_rope_rotate, (ctypes.byref(args), dt, x.shape[2], int(transpose), *tail,
+                                          x.shape[0], _stream(stream)), (args, keep))
+
+
+def jf_rope_rotate(rope: Rope, q, q_out, k=None, k_out=None, transpose: bool = False, stream=None):
+    """Rows q, k [total_tok][heads][d] (fp16 or bf16; parts of wider rows too) rotated into
+    q_out, k_out (which may be q, k); transpose: turned back, as gradients are."""
+    bind_rope_rotate(rope, q, q_out, k, k_out, transpose, stream)()
+
+
+def bind_kv8_rope_append(pool: KV8Pool, rope: Rope, k_new, v_new, cu_tok, start_pos, block_tables,
+                         q=None, q_out=None, stream=None) -> BoundCall:
+    """jf_kv8_rope_append with its arguments checked and marshalled once."""
+    _kv8_check(pool, (), ((cu_tok, "cu_tok"), (start_pos, "start_pos"), (block_tables, "block_tables")))
+    dt = _rope_type((k_new, "k_new"), (v_new, "v_new"), (q, "q"), (q_out, "q_out"))
+    lay, ptrs = pool.layout, pool.ptrs()
+    if tuple(k_new.shape[1:]) != (lay.num_kv_heads, lay.head_dim) or v_new.shape != k_new.shape:
+        raise ValueError("k_new/v_new must be [total_tok][Hkv][head_dim]")
+    n = k_new.shape[0]
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out are given both or neither")
+    if q is not None:
+        if q.dim() != 3 or (q.shape[0], q.shape[2]) != (n, lay.head_dim) or q_out.shape != q.shape:
+            raise ValueError("q/q_out must be [total_tok][Hq][head_dim]")
+        _dev_check(q_out, "q_out")
+    B = start_pos.shape[0]
+    _kv8_tables(block_tables, B)
+    if tuple(cu_tok.shape) != (B + 1,):
+        raise ValueError("cu_tok must be [B+1]")
+    turn = rope.args(n)
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), dt, ctypes.byref(turn), _ptr(k_new),
+            _rope_stride(k_new, "k_new"), _ptr(v_new), _rope_stride(v_new, "v_new"), _ptr(q),
+            0 if q is None else _rope_stride(q, "q"), _ptr(q_out), 0 if q is None else q.shape[1],
+            _ptr(cu_tok), _ptr(start_pos), _ptr(block_tables), B, block_tables.shape[1], n,
+            _stream(stream))
+    return BoundCall(lib.jf_kv8_rope_append, args,
+                     (lay, ptrs, turn, pool, rope, k_new, v_new, cu_tok, start_pos, block_tables, q, q_out))
+
+
+def jf_kv8_rope_append(pool: KV8Pool, rope: Rope, k_new, v_new, cu_tok, start_pos, block_tables,
+                       q=None, q_out=None, stream=None):
+    """Rows k_new (rotated on the way) and v_new [total_tok][Hkv][d] into an 8-bit cache at
+    their logical positions, and the same tokens' queries q [total_tok][Hq][d] rotated into
+    q_out, in one launch; k_new, v_new and q may be parts of wider rows."""
+    bind_kv8_rope_append(pool, rope, k_new, v_new, cu_tok, start_pos, block_tables, q, q_out, stream)()
