@@ -751,6 +751,42 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
                        void* workspace, size_t workspace_bytes, int32_t* kept,
                        float* kept_weights, hipStream_t stream);
 
+/* Decode attention of a batch whose requests share prefixes: as jf_kv8_decode_attn
+ * (the same queries, masks, types and limits), with the positions that a group's
+ * requests have in common read once for all of them.
+ *   group_start  int32 [num_groups + 1] (device): requests group_start[g] ..
+ *                group_start[g + 1] - 1 are group g; ascending from 0 to B (otherwise
+ *                every request is computed by itself).  Groups of one request, or none,
+ *                are allowed.
+ *   shared_lens  int32 [num_groups] (device): the first shared_lens[g] positions of
+ *                group g's requests hold the same keys and values.  They are read
+ *                through the table of the group's first request, and cut to its
+ *                length; what other tables hold for whole pages of them is not looked
+ *                at.  Any length will do, in the middle of a page too, 0 for none.
+ *   workspace    16-byte aligned device scratch of at least
+ *                jf_kv8_shared_workspace_bytes(); its contents do not matter before
+ *                the call nor after it.  Calls that may overlap in time, replays of
+ *                graphs among them, must not share one.
+ *   lse          NULL, or fp32 [B][num_queries][num_q_heads] (device): the natural
+ *                logarithm of the sum of exp(softmax_scale * q . k) over the positions
+ *                seen (-inf where there is none, for which out is zero)
+ * Lengths and groups are read on the device: a captured call can be replayed with
+ * others.  Two calls with the same inputs give the same bits; a request's results in
+ * another batch are the same up to the order of sums.  B <= 65,535,
+ * B * num_q_heads * num_queries <= 65,536, 1 <= num_groups <= B. */
+jf_status jf_kv8_shared_workspace_bytes(const jf_kv_layout* layout, int32_t B,
+                                        int32_t num_groups, int32_t num_queries,
+                                        int32_t num_q_heads, size_t* bytes);
+jf_status jf_kv8_shared_attn(const jf_kv_layout* layout,
+                             const jf_kv_pool_ptrs* pool, int32_t dtype,
+                             const void* q, int32_t B, int32_t num_queries,
+                             int32_t num_q_heads, const int32_t* block_tables,
+                             int32_t max_pages, const int32_t* seq_lens,
+                             const int32_t* group_start, const int32_t* shared_lens,
+                             int32_t num_groups, float softmax_scale, void* workspace,
+                             size_t workspace_bytes, void* out, float* lse,
+                             hipStream_t stream);
+
 /* ---------------------------------------------------- rotary positions
  * Rows of queries and keys rotated by their tokens' positions, as the models whose
  * caches this library keeps do before attention.  Of a head's dims the first rot_dim

@@ -192,6 +192,16 @@ hipError_t launch_kv8_evict(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, 
                             int32_t dst_pages, void* ws, int32_t* kept, float* kept_w,
                             hipStream_t stream);
 
+// Decode attention of requests in groups that share prefixes (kv8_shared.hip):
+// workspace bytes, and the launch (lse may be nullptr).
+size_t kv8_shared_bytes(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq);
+hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
+                             const void* q, int32_t B, int32_t sq, int32_t Hq,
+                             const int32_t* block_tables, int32_t max_pages, const int32_t* seq_lens,
+                             const int32_t* group_start, const int32_t* shared_lens, int32_t G,
+                             float softmax_scale, void* ws, void* out, float* lse,
+                             hipStream_t stream);
+
 // Read-rate calibration: one pass over bytes (a multiple of 16) of buf.
 hipError_t launch_read_stream(const void* buf, size_t bytes, int32_t blocks, uint32_t* sink,
                               hipStream_t stream);

@@ -36,6 +36,7 @@ EXPORTS = [
     "jf_kv8_prefill_workspace_bytes", "jf_kv8_prefill_attn", "jf_kv8_attn_weights",
     "jf_kv8_evict_workspace_bytes", "jf_kv8_evict",
     "jf_rope_frequencies", "jf_rope_table", "jf_rope_rotate", "jf_kv8_rope_append",
+    "jf_kv8_shared_workspace_bytes", "jf_kv8_shared_attn",
 ]
 
 
@@ -127,6 +128,9 @@ def _load():
                                      P]),
         "jf_kv8_evict_workspace_bytes": (st, [P, i32, i32, i32, ctypes.POINTER(sz)]),
         "jf_kv8_evict": (st, [P, P, i32, P, i32, P, P, i64, i32, i32, P, i32, P, sz, P, P, P]),
+        "jf_kv8_shared_workspace_bytes": (st, [P, i32, i32, i32, i32, ctypes.POINTER(sz)]),
+        "jf_kv8_shared_attn": (st, [P, P, i32, P, i32, i32, i32, P, i32, P, P, P, i32,
+                                    ctypes.c_float, P, sz, P, P, P]),
         "jf_rope_frequencies": (st, [i32, ctypes.c_double, i32, ctypes.c_double, i32,
                                      ctypes.c_double, ctypes.c_double, P, P]),
         "jf_rope_table": (st, [P, i32, P, i32, ctypes.c_float, P, P]),
@@ -1080,6 +1084,46 @@ def jf_kv8_evict(pool: KV8Pool, block_tables, seq_lens, weights, keep: int, rece
     capacity, zeros behind."""
     bind_kv8_evict(pool, block_tables, seq_lens, weights, keep, recent, dst_tables, workspace, kept,
                    kept_weights, stream)()
+
+
+def jf_kv8_shared_workspace_bytes(lay: Layout, B: int, num_groups: int, num_queries: int,
+                                  num_q_heads: int) -> int:
+    return _size(lib.jf_kv8_shared_workspace_bytes, ctypes.byref(lay), B, num_groups, num_queries,
+                 num_q_heads)
+
+
+def bind_kv8_shared(pool: KV8Pool, q, block_tables, seq_lens, group_start, shared_lens, softmax_scale,
+                    workspace, out, lse=None, stream=None) -> BoundCall:
+    """jf_kv8_shared_attn with its arguments checked and marshalled once."""
+    dt = _kv8_check(pool, ((q, "q"), (out, "out")),
+                    ((block_tables, "block_tables"), (seq_lens, "seq_lens"),
+                     (group_start, "group_start"), (shared_lens, "shared_lens")),
+                    ((lse, "lse"),), ((workspace, "workspace"),))
+    lay, ptrs = pool.layout, pool.ptrs()
+    if q.dim() != 4 or q.shape[3] != lay.head_dim or out.shape != q.shape:
+        raise ValueError("q/out must be [B][Sq][Hq][head_dim]")
+    B, Sq, Hq, _ = q.shape
+    _kv8_tables(block_tables, B, seq_lens)
+    if shared_lens.dim() != 1 or tuple(group_start.shape) != (shared_lens.shape[0] + 1,):
+        raise ValueError("shared_lens must be [groups], group_start [groups + 1]")
+    if lse is not None and lse.shape != q.shape[:3]:
+        raise ValueError("lse must be [B][Sq][Hq]")
+    args = (ctypes.byref(lay), ctypes.byref(ptrs), dt, _ptr(q), B, Sq, Hq, _ptr(block_tables),
+            block_tables.shape[1], _ptr(seq_lens), _ptr(group_start), _ptr(shared_lens),
+            shared_lens.shape[0], float(softmax_scale), _ptr(workspace), _nbytes(workspace), _ptr(out),
+            _ptr(lse), _stream(stream))
+    return BoundCall(lib.jf_kv8_shared_attn, args, (lay, ptrs, pool, q, block_tables, seq_lens,
+                                                    group_start, shared_lens, workspace, out, lse))
+
+
+def jf_kv8_shared_attn(pool: KV8Pool, q, block_tables, seq_lens, group_start, shared_lens,
+                       softmax_scale: float, workspace, out, lse=None, stream=None):
+    """Decode over the 8-bit cache of requests in groups (group_start int32 [groups + 1])
+    whose first shared_lens int32 [groups] positions are the same, read once for all of
+    a group: q, out [B][Sq][Hq][d], Sq = 1..4 causal tokens at the end of each request,
+    lse fp32 [B][Sq][Hq]."""
+    bind_kv8_shared(pool, q, block_tables, seq_lens, group_start, shared_lens, softmax_scale,
+                    workspace, out, lse, stream)()
 
 
 # ------------------------------------------------------- rotary positions
