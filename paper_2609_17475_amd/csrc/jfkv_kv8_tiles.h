@@ -1,0 +1,383 @@
+// The chunk attention's walk over tiles of 64 positions (format: jfkv_kv8.h): a block of
+// eight waves, each with column sets of its own, over one KV head.  Shared by the
+// attention of a chunk and of requests that share prefixes; kv8_prefill.hip says what
+// bounds it.
+#pragma once
+
+#include <type_traits>
+
+#include "jfkv_kv8.h"
+
+namespace jfkv {
+namespace kv8 {
+namespace tiles {
+
+#define JF_INLINE __attribute__((always_inline))
+
+constexpr int kTile = 64;        // positions of a tile (in one page)
+constexpr int kWaves = 8;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kFar = 4;          // tiles by which lines are touched ahead of their fetch
+constexpr uint32_t kZeroExp = 1;  // the exponent byte of a block of zeros
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// The query row of (row, head) as B operands: dims 64 c + 16 g + 8 j ..
+template <int C, bool BF16>
+__device__ __forceinline__ void load_q(u32x4 (&qf)[C][2], const uint16_t* qp, int g, uint32_t flip) {
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      qf[c][j] = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j) ^ flip;
+}
+
+// Tiles j0 .. j1 - 1 of a KV head for the columns of the block's waves: NC sets of 16 a
+// wave, whose queries are qf and which see the positions below see (`least`: the least
+// of the wave's).  L: positions that are written.  A tile's K and V codes are fetched
+// into registers two tiles ahead, widened once for the block and laid into LDS as the
+// matrix operands that all waves read.  acc (in units of 2^e_ref), m and l (log2 units)
+// grow.  Waves that are not active only carry.  table: a pointer to int32.
+template <int D, bool BF16, int NC, class Table, class Sees>
+__device__ __forceinline__ void walk_tiles(
+    const uint8_t* k_codes, const uint8_t* k_exps,
+    const uint8_t* v_codes, const uint8_t* v_exps,
+    int tid, Table table, int Hkv, int kv, int P, int block_shift, int num_pages, int L,
+    int j0, int j1, float scale_log2, const u32x4 (&qf)[NC][D / 64][2], const Sees& sees,
+    bool active, u32x4 (*tiles_k)[8 * D], u32x4 (*tiles_v)[8 * D],
+    f32x4 (&acc)[NC][D / 64][4], float (&m)[NC], float (&l)[NC], int& e_ref, int& e_top) {
+  constexpr int C = D / 64;
+  const int lane = tid & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // ---- tile transport: K's codes are fetched two tiles ahead and go to LDS one
+  // tile ahead, V's one tile later each
+  constexpr int kPieces = 4 * D / kThreads > 0 ? 4 * D / kThreads : 1;  // of 16 bytes per thread
+  constexpr int kOf = 4 * D < kThreads ? 4 * D : kThreads;              // threads that take some
+  u32x4 k_stage[kPieces], v_stage[kPieces];
+  uint32_t exps = 0, exps_next = 0;  // lanes 0..3: K's exponent bytes of a tile, 4..7: V's
+  // the place of a tile, stepped without divisions
+  struct Place {
+    int page, slot;
+  };
+  const int last_page = (j1 * kTile - 1) / P;
+  auto step = [&](Place& at) JF_INLINE {
+    at.slot += kTile;
+    if (at.slot == P) at.slot = 0, ++at.page;
+  };
+  auto page_of = [&](const Place& at) JF_INLINE { return table[min(at.page, last_page)]; };
+  // A tile without a page in the pool travels as page 0's, but counts as a tile of
+  // zeros that nobody sees: page 0's codes may be NaN and its exponents are someone
+  // else's.  (Its values are cleared by a mask on every tile.  Times against none at
+  // all, 2,048 rows over 65,536 positions and, d = 256, 256 over 196,608: 0.96 and
+  // 0.99; with a branch around the mask 1.00 and 1.02, around the products instead
+  // 1.01 and 1.00.)
+  auto held = [&](int pid) JF_INLINE { return (uint32_t)pid < (uint32_t)num_pages; };
+  auto run_of = [&](int pid) JF_INLINE { return (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv; };
+  const uint32_t k_off = (tid / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
+  auto fetch_k = [&](int slot0, int pid) JF_INLINE {
+    const size_t run = run_of(pid);
+    const uint8_t* kp = k_codes + (run * P + slot0) * D;
+    if (kOf == kThreads || tid < kOf) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        k_stage[k] = *reinterpret_cast<const u32x4*>(kp + k_off + k * (kThreads / D) * 16 * D);
+    }
+    const uint8_t* ep = (lane & 4) ? v_exps : k_exps;
+    exps_next = ep[run * (P >> block_shift) + ((slot0 + 16 * (lane & 3)) >> block_shift)];
+  };
+  auto fetch_v = [&](int slot0, int pid) JF_INLINE {
+    const uint8_t* vp = v_codes + (run_of(pid) * P + slot0) * D;
+    if (kOf == kThreads || tid < kOf) {
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k)
+        v_stage[k] = *reinterpret_cast<const u32x4*>(vp + (tid + k * kThreads) * 16);
+    }
+  };
+  auto deposit_k = [&](int j) JF_INLINE {
+    if (kOf < kThreads && tid >= kOf) return;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int i = tid + k * kThreads;
+      // [16 positions][64 dims][half][lane]
+      u32x4* to = tiles_k[j & 1] + i / 64 * 128 + i % 64;
+      to[0] = widen8<BF16>(k_stage[k].x, k_stage[k].y), to[64] = widen8<BF16>(k_stage[k].z, k_stage[k].w);
+    }
+  };
+  auto deposit_v = [&](int j, uint32_t keep) JF_INLINE {  // keep: all ones, or 0 without a page
+    if (kOf < kThreads && tid >= kOf) return;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int i = tid + k * kThreads;
+      v_stage[k] &= keep;
+      if ((j + 1) * kTile > L) {  // slots not written yet: zeros (their codes may be NaN)
+        const int left = min(max(L - (j * kTile + i / D * 16 + i % 64 / 16 * 4), 0), 4);
+        v_stage[k] &= left ? 0xffffffffu >> (8 * (4 - left)) : 0u;
+      }
+      // [32 positions][64 dims][dim % 4][lane][16 of the 32]
+      u32x2* to = reinterpret_cast<u32x2*>(tiles_v[j & 1] + (i / D / 2 * C + i % D / 64) * 256 + i % 64) + i / D % 2;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt) {
+        uint32_t lo, hi;
+        widen<false>(v_stage[k][dt], lo, hi);
+        to[dt * 128] = u32x2{lo, hi};
+      }
+    }
+  };
+
+  auto rescale = [&](float f) JF_INLINE {
+#pragma unroll
+    for (int cs = 0; cs < NC; ++cs)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= f;
+  };
+
+  // ---- a tile's three steps: scores (matrix cores), softmax (vector), values
+  // (matrix cores)
+  f32x4 s[4][NC];      // scores, times f[t] in log2 units
+  float f[4];
+  int ev[4];           // the values' exponents
+  uint32_t pf[2][NC][4];  // P as B operands
+  int split_e[4];      // where apart: the references of the tile's parts
+  bool apart = false;
+
+  // A run of operands that lie one after the other in LDS, each read kAhead
+  // before its products.  (The barriers keep the compiler from reading all of
+  // them at once, which spills.)
+  constexpr int kAhead = 4;
+  auto stream = [&](const u32x4* from, auto first, auto count, auto&& use) JF_INLINE {
+    constexpr int n0 = decltype(first)::value, nn = decltype(count)::value;
+    u32x4 ring[kAhead];
+#pragma unroll
+    for (int p = 0; p < kAhead; ++p) ring[p] = from[(n0 + p) * 64 + lane];
+#pragma unroll
+    for (int p = 0; p < nn; ++p) {
+      const u32x4 a = ring[p % kAhead];
+      if (p + kAhead < nn) ring[p % kAhead] = from[(n0 + p + kAhead) * 64 + lane];
+      use(n0 + p, a);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  auto scores = [&](int j) JF_INLINE {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int cs = 0; cs < NC; ++cs) s[t][cs] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      // (not 0, so that a hidden score times it stays -inf)
+      f[t] = fmaxf(scale_log2 * power2(__builtin_amdgcn_readlane((int)exps, t) - 127), 1e-37f);
+      ev[t] = __builtin_amdgcn_readlane((int)exps, 4 + t) - 127;
+    }
+    stream(tiles_k[j & 1], std::integral_constant<int, 0>{}, std::integral_constant<int, 8 * C>{},
+           [&](int p, u32x4 a) JF_INLINE {
+             const int t = p / (2 * C), c = p / 2 % C, half = p % 2;
+#pragma unroll
+             for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a, qf[cs][c][half], s[t][cs]);
+           });
+  };
+
+  auto softmax = [&](int j, bool on) JF_INLINE {
+    const int pos0 = j * kTile;
+    if (!on || sees.hides_some(pos0)) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (!on || sees.hides(cs, pos0 + 16 * t + 4 * g + i)) s[t][cs][i] = -INFINITY;
+        if (pos0 + 16 * t >= L) f[t] = 1.0f, ev[t] = ev[0];  // (exponents not written yet)
+      }
+    }
+    // maxima
+    float top[NC];
+    bool raise = false;
+#pragma unroll
+    for (int cs = 0; cs < NC; ++cs) {
+      top[cs] = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        top[cs] = larger(top[cs], f[t] * larger(larger(larger(s[t][cs][0], s[t][cs][1]),
+                                                       s[t][cs][2]), s[t][cs][3]));
+      raise |= top[cs] > m[cs] + kMargin;
+    }
+    if (__any(raise)) {
+#pragma unroll
+      for (int cs = 0; cs < NC; ++cs) {
+        const float mn = fmaxf(m[cs], col_max(top[cs]));
+        const float by = m[cs] == -INFINITY ? 0.0f : exp2_(m[cs] - mn);
+        l[cs] *= by;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int dt = 0; dt < 4; ++dt) acc[cs][c][dt] *= by;
+        m[cs] = mn;
+      }
+    }
+    float mu[NC];
+#pragma unroll
+    for (int cs = 0; cs < NC; ++cs) mu[cs] = m[cs] == -INFINITY ? 0.0f : m[cs];
+    int lo = ev[0], hi = ev[0];
+#pragma unroll
+    for (int t = 1; t < 4; ++t) lo = min(lo, ev[t]), hi = max(hi, ev[t]);
+    e_top = max(e_top, hi);
+    apart = hi - lo > kRefMax || lo < e_top - kRefFloor;
+    if (!apart) {
+      // one reference for the tile's values
+      if (lo < e_ref || hi > e_ref + kRefMax) {
+        const int e = max(hi - kRefMax, lo - 4);
+        rescale(reference_step(e_ref, e));
+        e_ref = e;
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) {
+          const float by = (float)(ev[t] - e_ref) - mu[cs];
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = exp2_(fmaf(s[t][cs][i], f[t], by));
+          l[cs] = fmaf((p[0] + p[1]) + (p[2] + p[3]), power2(e_ref - ev[t]), l[cs]);
+          pf[t / 2][cs][t % 2 * 2] = narrow2<false>(p[0], p[1]);
+          pf[t / 2][cs][t % 2 * 2 + 1] = narrow2<false>(p[2], p[3]);
+        }
+    } else {
+      // too far apart for that (or far below the largest values, where P may
+      // vanish and l must not): a reference for each 16 positions
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        split_e[t] = max(ev[t] - 4, e_top - kRefFloor);
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) {
+          const float by = (float)(ev[t] - split_e[t]) - mu[cs];
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = s[t][cs][i] * f[t];
+            p[i] = exp2_(x + by);
+            l[cs] += exp2_(x - mu[cs]);
+          }
+          pf[t / 2][cs][t % 2 * 2] = narrow2<false>(p[0], p[1]);
+          pf[t / 2][cs][t % 2 * 2 + 1] = narrow2<false>(p[2], p[3]);
+        }
+      }
+    }
+  };
+
+  auto values = [&](int j) JF_INLINE {
+    auto products = [&](auto t2, const u32x4 (&b)[NC]) {
+      stream(tiles_v[j & 1], std::integral_constant<int, decltype(t2)::value * 4 * C>{},
+             std::integral_constant<int, 4 * C>{}, [&](int p, u32x4 a) JF_INLINE {
+               const int c = p / 4 % C, dt = p % 4;
+#pragma unroll
+               for (int cs = 0; cs < NC; ++cs) acc[cs][c][dt] = mma<false>(a, b[cs], acc[cs][c][dt]);
+             });
+    };
+    constexpr std::integral_constant<int, 0> t0{};
+    constexpr std::integral_constant<int, 1> t1{};
+    if (!apart) {
+#pragma unroll
+      for (int t2 = 0; t2 < 2; ++t2) {
+        u32x4 b[NC];
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) b[cs] = u32x4{pf[t2][cs][0], pf[t2][cs][1], pf[t2][cs][2], pf[t2][cs][3]};
+        if (t2 == 0) products(t0, b); else products(t1, b);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        rescale(reference_step(e_ref, split_e[t]));
+        e_ref = split_e[t];
+        u32x4 b[NC];
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs)
+          b[cs] = t % 2 ? u32x4{0u, 0u, pf[t / 2][cs][2], pf[t / 2][cs][3]}
+                        : u32x4{pf[t / 2][cs][0], pf[t / 2][cs][1], 0u, 0u};
+        if (t < 2) products(t0, b); else products(t1, b);
+      }
+    }
+  };
+
+  // ---- Turn j forms the scores of tile j and the value products of tile j - 1.
+  // Waves w and w + 4 share a SIMD: the first do their matrix products at once and
+  // the vector work (the softmax, the next tiles' way into LDS) after them, the
+  // second the other way round, so that one's matrix products meet the other's
+  // vector work (d = 256: 256 rows over 196,608 positions 1,790 -> 1,430 us; at d =
+  // 64, where the vector work is the most, all do the same).  (Two loops, as one loop
+  // with both orders spills; every wave passes j1 - j0 + 1 barriers in either.)
+  auto walk = [&](auto is_late) JF_INLINE {
+    constexpr bool late = decltype(is_late)::value;
+    Place at = {j0 * kTile / P, j0 * kTile % P};
+    int pid[4], slot[4];  // of tiles j - 1, j, j + 1, j + 2
+    pid[0] = -1, slot[0] = 0;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      pid[i] = page_of(at), slot[i] = at.slot;
+      step(at);
+    }
+    fetch_k(slot[1], pid[1]);
+    exps = held(pid[1]) ? exps_next : kZeroExp;
+    deposit_k(j0);
+    fetch_v(slot[1], pid[1]);
+    fetch_k(slot[2], pid[2]);
+    // kFar tiles further ahead each line is touched once, so that the fetches find
+    // it in the L2 (2,048 rows over 65,536 positions that the last-level cache does
+    // not hold: 2,815 -> 2,540 us)
+    Place far = at;
+#pragma unroll
+    for (int i = 0; i < kFar; ++i) step(far);
+    int pid_far = page_of(far), slot_far = far.slot;
+    uint32_t touched = 0;
+    for (int j = j0; j <= j1; ++j) {
+      __syncthreads();  // K of tile j and V of tile j - 1 are in LDS
+      const int pid_n = page_of(at);
+      if (tid < D) {
+        asm volatile("" ::"v"(touched));
+        const uint8_t* from = (tid < D / 2 ? k_codes : v_codes) + (run_of(pid_far) * P + slot_far) * D;
+        touched = *reinterpret_cast<const uint32_t*>(from + tid % (D / 2) * 128);
+      }
+      step(far);
+      pid_far = page_of(far), slot_far = far.slot;
+      uint32_t exps_1 = exps_next;
+      auto transport = [&]() JF_INLINE {
+        if (j < j1) {
+          deposit_v(j, held(pid[1]) ? 0xffffffffu : 0u);
+          fetch_v(slot[2], pid[2]);
+        }
+        if (j + 1 < j1) {
+          deposit_k(j + 1);
+          fetch_k(slot[3], pid[3]);
+        }
+      };
+      if constexpr (late) {
+        if (active && j > j0) softmax(j - 1, (uint32_t)pid[0] < (uint32_t)num_pages);
+        transport();
+      }
+      __builtin_amdgcn_s_setprio(1);
+      if (active) {
+        if (j > j0) values(j - 1);
+        if (j < j1) scores(j);
+      }
+      __builtin_amdgcn_s_setprio(0);
+      if constexpr (!late) {
+        if (active && j < j1) softmax(j, (uint32_t)pid[1] < (uint32_t)num_pages);
+        transport();
+      }
+      exps = held(pid[2]) ? exps_1 : kZeroExp;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) pid[i] = pid[i + 1], slot[i] = slot[i + 1];
+      pid[3] = pid_n, slot[3] = at.slot;
+      step(at);
+    }
+  };
+  if (j0 < j1) {
+    if (D > 64 && wave >= kWaves / 2)
+      walk(std::true_type{});
+    else
+      walk(std::false_type{});
+  }
+}
+
+}  // namespace tiles
+}  // namespace kv8
+}  // namespace jfkv

@@ -10,41 +10,56 @@
 //
 // The (request, token, head) triples that read a KV head are the columns of the
 // matrix products, 16 to a set, and what kv8_decode.hip says of operands, exponents
-// and roundings holds here too; with more sets per wave a widened code serves more
-// products.  The work is a line of units: for each group its chunks of columns and KV
-// heads, then for each request its own positions and KV heads; a unit is a run of rows
-// of 32 positions.  The line is cut into pieces of equal cost, a block each, wherever
-// that falls, so that all CUs end together and products (groups) meet loads (requests);
-// each (block, unit) leaves one record, which a second launch joins.
+// and roundings holds here too.  Two kernels: one walks rows of 32 positions, each wave
+// its own (requests' own positions, groups of few columns; bound by HBM), one walks
+// tiles of 64 positions, each wave with columns of its own (groups of many columns;
+// bound by the vector work beside the matrix cores, as the chunk attention).  The work
+// of either is a line of units: for each group its chunks of columns and KV heads, then
+// for each request its KV heads; a unit is a run of steps over positions.  The line is
+// cut into pieces of equal cost, a block each, wherever that falls; each (block, unit)
+// leaves one record, which a last launch joins.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "jfkv_internal.h"
 #include "jfkv_kv8.h"
+#include "jfkv_kv8_tiles.h"
 
 namespace jfkv {
 namespace {
 
 using namespace kv8;
+using tiles::kTile;
+using tiles::walk_tiles;
 
-constexpr int kWaves = 8;
-constexpr int kThreads = 64 * kWaves;
-constexpr int kRow = 32;       // positions a wave takes at a time (in one page)
-constexpr int kMinRows = 3;    // rows per wave below which a unit is not cut
-constexpr int kGroupsLds = 512;
+constexpr int kRow = 32;        // positions that a wave of the row walk takes at a time (in one page)
+constexpr int kRowWaves = 4;
+constexpr int kRowBlocks = 2;   // blocks of the row walk per CU
+constexpr int kRowThreads = 64 * kRowWaves, kTileThreads = tiles::kThreads;
+constexpr int kMinRows = 2;     // rows per wave below which a unit is not cut
+constexpr int kRowCols = 64;    // columns of a group that are walked by rows at most
+constexpr int kSub = 32;        // columns that can have a chunk of their own
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// Sets of 16 columns of a chunk: what the accumulators leave room for.
-template <int D>
-constexpr int max_sets() {
-  return 2;
+// How a chunk of columns is computed: by rows, one or two sets of 16 columns for all of
+// a block's waves, or by tiles, one or two sets for each of eight waves.
+enum Kind { kRows1, kRows2, kTiles1, kTiles2 };
+__host__ __device__ constexpr int widest(int D) { return D > 128 ? 128 : 256; }
+__host__ __device__ constexpr int width_log2(int kind) {
+  return kind == kRows1 ? 4 : kind == kRows2 ? 5 : kind == kTiles1 ? 7 : 8;
 }
-__host__ __device__ constexpr int sets_for(int D, int cols) {
-  return cols <= 16 ? 1 : 2;
+__host__ __device__ constexpr int width_of(int kind) { return 1 << width_log2(kind); }
+__host__ __device__ constexpr int step_log2(int kind) { return kind >= kTiles1 ? 6 : 5; }
+__host__ __device__ constexpr int kind_of(int D, int cols) {
+  return cols <= 16 ? kRows1 : cols <= kRowCols ? kRows2 : cols <= 128 || D > 128 ? kTiles1 : kTiles2;
 }
-// Cost of a row of 32 positions by its sets.
-__host__ __device__ constexpr int row_cost(int sets) { return sets > 2 ? 3 : 2; }
+// Cost of a step, and of a unit's start and end, in about 0.1 us of a block.
+__host__ __device__ constexpr int cost_of(int kind) {
+  return kind == kRows1 ? 4 : kind == kRows2 ? 5 : kind == kTiles1 ? 16 : 24;
+}
+__host__ __device__ constexpr int start_of(int kind) { return kind >= kTiles1 ? 60 : 30; }
 
 // Values that are the same in all lanes, to scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -53,81 +68,301 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 }
 
 // What a walk reads.  (Kernel arguments of their own: the compiler then knows that no
-// store meets them, and reads the tables by scalar loads.)
+// store meets them.)
 struct Cache {
   const uint8_t *k_codes, *k_exps, *v_codes, *v_exps;
   const uint16_t* q;
-  const int32_t *tables, *lens;
+  const int32_t* tables;
 };
 struct Args {
   const int32_t *first, *shared;
   int2* info;     // (first record, records) of each unit: groups', then requests'
-  int B, G, sq, Hq, Hkv, P, block_shift, num_pages, max_pages;
-  int group_units, chunks, own_cols;  // chunks and columns of a request's own units
-  int64_t own_recs;                   // where requests' records begin (floats)
+  int B, G, sq, Hq, Hkv, gq, P, block_shift, num_pages, max_pages;
+  int group_units, own_kind, chunks, own_cols;  // kind, chunks and columns of a request's own units
+  int64_t row_recs, own_recs;  // where groups' records by rows and requests' records begin (floats)
   float scale_log2;
+  uint32_t flip;  // a negative scale negates the queries instead
 };
 
-// The groups, from LDS where they fit: valid only if their bounds ascend from 0 to B.
-struct Groups {
-  const int32_t *first, *shared;
-  int n;
-  bool valid;
+// floor(y / d) for 0 <= y < 2^53 and 0 < d: the nearest quotient of two whole numbers does
+// not reach the next whole number.  (Some twenty instructions; a division of 64-bit
+// integers has over a hundred.)
+__device__ __forceinline__ int64_t whole(int64_t y, int64_t d) {
+  return (int64_t)floor((double)y / (double)d);
+}
+
+// Groups and lengths, from LDS where they fit.  The groups are valid only if their
+// bounds ascend from 0 to B.
+struct Batch {
+  const int32_t *g_first, *g_shared, *g_lens;
+  const int32_t *s_first, *s_shared, *s_lens;
+  int groups, cap;
+  bool in_lds, valid;
+  __device__ __forceinline__ int first(int g) const { return in_lds ? s_first[g] : g_first[g]; }
+  __device__ __forceinline__ int length(int b) const {
+    return min(max(in_lds ? s_lens[b] : g_lens[b], 0), cap);
+  }
   // the group of request b
   __device__ __forceinline__ int of(int b) const {
-    int lo = 0, hi = n;
+    int lo = 0, hi = groups;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      if (first[mid] <= b) lo = mid; else hi = mid;
+      if (first(mid) <= b) lo = mid; else hi = mid;
     }
     return lo;
   }
-};
-
-__device__ __forceinline__ int length_of(const Args& a, const int32_t* lens, int b) {
-  return min(max(lens[b], 0), a.max_pages * a.P);
-}
-// Positions that group g's requests share (none for a request alone): those that its
-// first request, whose table is read, has.
-__device__ __forceinline__ int shared_of(const Args& a, const int32_t* lens, const Groups& gr, int g) {
-  if (!gr.valid || gr.first[g + 1] - gr.first[g] < 2) return 0;
-  return min(max(gr.shared[g], 0), length_of(a, lens, gr.first[g]));
-}
-__device__ __forceinline__ int own_start(const Args& a, const int32_t* lens, const Groups& gr, int b) {
-  return gr.valid ? shared_of(a, lens, gr, gr.of(b)) : 0;
-}
-
-// An item of the line: a group's shared positions or a request's own ones.
-struct Item {
-  int request, requests;  // the first one, whose table is read, and how many
-  int lo, hi;             // positions
-  int sets, chunks, rows;
-  int unit;               // number of its first unit
-};
-template <int D>
-__device__ __forceinline__ Item item_of(const Args& a, const int32_t* lens, const Groups& gr, int i) {
-  Item t;
-  const int pairs = a.Hq / a.Hkv * a.sq;
-  if (i < a.G) {
-    t.request = gr.valid ? gr.first[i] : 0;
-    t.requests = gr.valid ? gr.first[i + 1] - t.request : 0;
-    t.lo = 0, t.hi = shared_of(a, lens, gr, i);
-    t.sets = sets_for(D, t.requests * pairs);
-    t.chunks = (t.requests * pairs + 16 * t.sets - 1) / (16 * t.sets);
-    t.unit = (t.request * pairs / (16 * max_sets<D>()) + i) * a.Hkv;
-  } else {
-    t.request = i - a.G, t.requests = 1;
-    t.lo = own_start(a, lens, gr, t.request), t.hi = length_of(a, lens, t.request);
-    t.sets = sets_for(D, a.own_cols);
-    t.chunks = a.chunks;
-    t.unit = a.group_units + t.request * a.chunks * a.Hkv;
+  // Positions that group g's requests share (none for a request alone): those that its
+  // first request, whose table is read, has.
+  __device__ __forceinline__ int shared(int g) const {
+    const int b = first(g);
+    if (!valid || first(g + 1) - b < 2) return 0;
+    return min(max(in_lds ? s_shared[g] : g_shared[g], 0), length(b));
   }
-  t.rows = t.hi > t.lo ? (t.hi + kRow - 1) / kRow - t.lo / kRow : 0;
+};
+
+// An item of the line: the full chunks of a group's columns over its shared positions
+// (items 2 g), the other columns (2 g + 1), or a request's own positions.
+struct Item {
+  int request;     // the first one, whose table is read
+  int col0, cols;  // columns, counted from that request's first
+  int lo, hi;      // positions
+  int kind;
+  __device__ __forceinline__ int chunks() const {
+    return (cols - col0 + width_of(kind) - 1) >> width_log2(kind);
+  }
+  __device__ __forceinline__ int steps() const {
+    const int s = step_log2(kind);
+    return hi > lo ? ((hi - 1) >> s) - (lo >> s) + 1 : 0;
+  }
+  // cost of a unit but for its start
+  __device__ __forceinline__ int64_t work() const { return (int64_t)steps() * cost_of(kind); }
+};
+// (An item of the other kernel is empty.)
+template <int D, bool TILES>
+__device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i) {
+  Item t;
+  const int pairs = a.gq * a.sq;
+  if (i < 2 * a.G) {
+    constexpr int W = widest(D);
+    const int g = i >> 1;
+    t.request = batch.first(g);
+    const int cols = batch.valid ? (batch.first(g + 1) - t.request) * pairs : 0, full = cols & -W;
+    t.col0 = i & 1 ? full : 0;
+    t.cols = i & 1 ? cols : full;
+    t.kind = i & 1 ? kind_of(D, cols - full) : kind_of(D, W);
+    t.lo = 0;
+    t.hi = t.cols > t.col0 && (t.kind >= kTiles1) == TILES ? batch.shared(g) : 0;
+  } else {
+    t.request = i - 2 * a.G;
+    t.col0 = 0, t.cols = pairs;
+    t.lo = batch.valid ? batch.shared(batch.of(t.request)) : 0, t.hi = batch.length(t.request);
+    t.kind = a.own_kind;
+  }
   return t;
 }
-__device__ __forceinline__ int64_t work_of(const Args& a, const Item& t) {
-  return (int64_t)t.rows * row_cost(t.sets) * t.chunks * a.Hkv;
+
+// How the line is cut.  Where units are few, each begins a piece of its own and its
+// length is rounded up to whole pieces, so that no block starts twice; else units
+// follow one another, each with its start's cost.
+struct Line {
+  int64_t piece;
+  bool apart;
+  __device__ __forceinline__ int64_t span(const Item& t) const {
+    const int64_t work = t.work();
+    if (!work) return 0;
+    return apart ? (whole(work - 1, piece) + 1) * piece : start_of(t.kind) + work;
+  }
+};
+// A chunk's record slot, its first column there, and its entry of `info`, for a KV head:
+// of a group's columns from `col` on, the group's first request and number given, ..
+template <int D>
+__device__ __forceinline__ void group_place(const Args& a, int request, int g, int col, int kv, int& id,
+                                            int& at, int& entry) {
+  constexpr int W = widest(D);
+  id = (request * a.gq * a.sq / W + g + col / W) * a.Hkv + kv;
+  at = col % W, entry = id * (W / kSub) + at / kSub;
 }
+// .. and of a request's own.
+template <int D>
+__device__ __forceinline__ void own_place(const Args& a, int request, int chunk, int kv, int& id, int& entry) {
+  id = (request * a.chunks + chunk) * a.Hkv + kv;
+  entry = a.group_units * (widest(D) / kSub) + id;
+}
+
+// Where a block is on the line: at x, up to end; the window of items that is summed up
+// begins with item `window`.
+struct State {
+  int64_t x, end;
+  int window;
+  bool valid;
+};
+// Steps r0 .. r1 - 1 of a unit: its chunk's first column, KV head and record.
+struct Segment {
+  Item it;
+  int col, kv, r0, r1;
+  int64_t rec;
+};
+// The plan of a block of T threads.  (What lives from one segment to the next is in LDS,
+// so that the walks have the registers.)
+template <int T>
+struct Plan {
+  Args a;
+  Line line;
+  State state;
+  Segment segment;
+  int64_t upto[T + 1];  // the line up to the window's item i, itself among it: upto[i + 1]
+  Item items[T];
+  int64_t sum[T / 64];
+  int units[T / 64], starts[T / 64];
+  int32_t first[T + 1], shared[T], lens[2 * T];
+
+  __device__ __forceinline__ Batch batch(const Args& g, const int32_t* g_lens, bool valid) const {
+    return Batch{g.first, g.shared, g_lens, first, shared, lens, g.G, g.max_pages * g.P,
+                 g.G <= T && g.B <= 2 * T, valid};
+  }
+
+  // All threads; false: nothing for this block.
+  template <int D, bool TILES>
+  __device__ __forceinline__ bool begin(const Args& g, const int32_t* g_lens) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), blocks = gridDim.x;
+    Batch b = batch(g, g_lens, true);
+    int bad = 0;
+    for (int i = tid; i <= g.G; i += T) {
+      const int at = g.first[i];
+      bad |= i == 0 ? at != 0 : at < g.first[i - 1];
+      if (i == g.G) bad |= at != g.B;
+      if (b.in_lds) {
+        first[i] = at;
+        if (i < g.G) shared[i] = g.shared[i];
+      }
+    }
+    if (b.in_lds)
+      for (int i = tid; i < g.B; i += T) lens[i] = g_lens[i];
+    b.valid = !__syncthreads_or(bad);
+
+    const int n = TILES ? 2 * g.G : 2 * g.G + g.B;
+    int64_t work = 0;
+    int count = 0, begins = 0;
+    for (int i = tid; i < n; i += T) {
+      const Item t = item_of<D, TILES>(g, b, i);
+      const int64_t w = t.work();
+      const int m = w ? t.chunks() * g.Hkv : 0;
+      work += w * m, count += m, begins += m * start_of(t.kind);
+      items[tid] = t;
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1)
+      work += __shfl_xor(work, o), count += __shfl_xor(count, o), begins += __shfl_xor(begins, o);
+    if (lane == 0) sum[wave] = work, units[wave] = count, starts[wave] = begins;
+    __syncthreads();
+    work = 0, count = begins = 0;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) work += sum[w], count += units[w], begins += starts[w];
+    work = uniform(work), count = uniform(count), begins = uniform(begins);
+    constexpr int64_t kLeast = TILES ? 2 * cost_of(kTiles1) : cost_of(kRows1) * kRowWaves * kMinRows;
+    Line l;
+    l.apart = 2 * count <= blocks;
+    l.piece = max(l.apart ? whole(work, blocks - count) + 1 : whole(work + begins, blocks) + 1, kLeast);
+    const int64_t from = blockIdx.x * l.piece;
+    // (no more than this is behind: the line's own end is known with its last item)
+    if (from >= (l.apart ? work + count * l.piece : work + begins)) return false;
+    if (tid == 0) {
+      a = g, line = l;
+      state = State{from, from + l.piece, -T, b.valid};
+      upto[T] = 0;  // (no window yet)
+    }
+    __syncthreads();
+    return true;
+  }
+
+  // All threads: the block's next segment; false: none is left.
+  template <int D, bool TILES>
+  __device__ __forceinline__ bool next(const int32_t* g_lens) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int lane = tid & 63, wave = uniform(tid >> 6);
+    const int n = uniform(TILES ? 2 * a.G : 2 * a.G + a.B);
+    for (;;) {
+      const int64_t x = uniform(state.x);
+      int window = uniform(state.window);
+      if (x >= uniform(state.end)) return false;
+      while (x >= uniform(upto[T])) {
+        const int64_t carry = uniform(upto[T]);
+        window += T;
+        if (window >= n) return false;
+        const bool mine = window + tid < n;
+        if (n > T && mine) items[tid] = item_of<D, TILES>(a, batch(a, g_lens, state.valid), window + tid);
+        int64_t to = 0;
+        if (mine) {
+          const Item t = items[tid];
+          to = line.span(t) * (t.chunks() * a.Hkv);
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+          const int64_t up = __shfl_up(to, o);
+          if (lane >= o) to += up;
+        }
+        if (lane == 63) sum[wave] = to;
+        __syncthreads();
+        to += carry;
+#pragma unroll
+        for (int w = 0; w < T / 64; ++w) to += w < wave ? sum[w] : 0;
+        upto[tid + 1] = to;
+        if (tid == 0) upto[0] = carry, state.window = window;
+        __syncthreads();
+      }
+      __syncthreads();
+      if (x >= upto[tid] && x < upto[tid + 1]) {  // one thread's item
+        // the unit, and its steps that begin in the block's piece
+        const Item it = items[tid];
+        const Line l = line;
+        const int cost = cost_of(it.kind), steps = it.steps();
+        const int64_t span = l.span(it), end = state.end;
+        const int u = (int)whole(x - upto[tid], span);
+        const int64_t start = upto[tid] + u * span, at = start + (l.apart ? 0 : start_of(it.kind));
+        const int r0 = (int)whole(max(x - at, (int64_t)0) + cost - 1, cost);
+        const int r1 = min(steps, (int)whole(max(end - at, (int64_t)0) + cost - 1, cost));
+        const int chunk = (int)((uint32_t)u / (uint32_t)a.Hkv), kv = u - chunk * a.Hkv;
+        const int i = window + tid, col = it.col0 + (chunk << width_log2(it.kind));
+        int id, first_col, entry;
+        int64_t rec;
+        if (TILES || i < 2 * a.G) {
+          group_place<D>(a, it.request, i >> 1, col, kv, id, first_col, entry);
+          const int64_t slot = (int64_t)id + blockIdx.x;
+          rec = (TILES ? slot * widest(D) + first_col : a.row_recs / (D + 4) + slot * kRowCols + first_col % kRowCols) * (D + 4);
+        } else {
+          own_place<D>(a, it.request, chunk, kv, id, entry);
+          rec = a.own_recs + ((int64_t)id + blockIdx.x) * (a.own_cols * (D + 4));
+        }
+        if (r0 == 0 && r1 > 0) {
+          const int from = (int)whole(at, l.piece), to = (int)whole(at + it.work() - cost, l.piece);
+          a.info[entry] = make_int2(id + from, to - from + 1);
+        }
+        segment = Segment{it, col, kv, r0, r1, rec};
+        state.x = start + span;
+      }
+      __syncthreads();
+      if (uniform(segment.r0) < uniform(segment.r1)) return true;  // (else a unit's start alone)
+    }
+  }
+
+  // The arguments and the segment, in scalar registers.
+  __device__ __forceinline__ Args args() const {
+    Args f = a;
+    f.sq = uniform(f.sq), f.Hq = uniform(f.Hq), f.Hkv = uniform(f.Hkv), f.gq = uniform(f.gq);
+    f.P = uniform(f.P), f.block_shift = uniform(f.block_shift), f.num_pages = uniform(f.num_pages);
+    f.max_pages = uniform(f.max_pages), f.flip = uniform((int)f.flip);
+    f.scale_log2 = __uint_as_float(uniform((int)__float_as_uint(f.scale_log2)));
+    return f;
+  }
+  __device__ __forceinline__ Segment part() const {
+    Segment t = segment;
+    t.it.request = uniform(t.it.request), t.it.cols = uniform(t.it.cols), t.it.lo = uniform(t.it.lo);
+    t.it.hi = uniform(t.it.hi), t.it.kind = uniform(t.it.kind), t.col = uniform(t.col);
+    t.kv = uniform(t.kv), t.r0 = uniform(t.r0), t.r1 = uniform(t.r1), t.rec = uniform(t.rec);
+    return t;
+  }
+};
 
 template <int D>
 struct Row {
@@ -135,60 +370,42 @@ struct Row {
   uint32_t exps;  // lanes 0, 1: K's exponent bytes of the two tiles; 2, 3: V's
 };
 
-// Rows r0 .. r1 - 1 (counted from the item's first) of one unit: its record to rec.
+// What column `col` of an item's request reads: its query, and how many positions.
+template <int D>
+__device__ __forceinline__ const uint16_t* query_of(const Args& a, const Cache& in, const Batch& batch, const Item& it,
+                                                    int col, int kv, int& see) {
+  const int row = col / a.gq;
+  see = min(batch.length(it.request + row / a.sq) - a.sq + 1 + row % a.sq, it.hi);
+  return in.q + (((size_t)it.request * a.sq + row) * a.Hq + kv * a.gq + col % a.gq) * D;
+}
+
+// The pages of an item: constant memory as far as the kernel goes, read by scalar loads.
+typedef const __attribute__((address_space(4))) int32_t* Table;
+__device__ __forceinline__ Table table_of(const Args& a, const Cache& in, const Item& it) {
+  return (Table)(uintptr_t)(in.tables + (size_t)it.request * a.max_pages);
+}
+
+// Steps r0 .. r1 - 1 (counted from the item's first) of the chunk of columns from c0 on,
+// its record to rec, by rows.
 template <int D, bool BF16, int CS>
-__device__ __forceinline__ void walk(const Args& a, const Cache& in, const Item& it, int chunk, int kv, int r0, int r1,
-                                     float* rec, float* smem) {
+__device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const Batch& batch,
+                                          const Item& it, int c0, int kv,
+                                          int r0, int r1, float* rec, float* smem) {
   constexpr int C = D / 64;
   constexpr int kPart = D + 4;  // floats of a partial: o, m, l (16-byte rows)
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int gq = a.Hq / a.Hkv, P = a.P;
-  const int c0 = chunk * 16 * CS, ncols = min(16 * CS, it.requests * a.sq * gq - c0);
+  const int P = a.P, ncols = min(16 * CS, it.cols - c0);
 
-  // ---- queries as B operands: column n of each set, dims 64 c + 16 g + 8 j .., in
-  // registers or, where they would fill them, in LDS
-  constexpr bool kQLds = CS > 1;
-  int see[CS], least = 0x7fffffff;  // positions the columns' queries see
-  u32x4 qf[CS][C][2];
-  u32x4* const s_q = reinterpret_cast<u32x4*>(smem);
-  __syncthreads();  // (LDS still holds what was before)
-#pragma unroll
-  for (int cs = 0; cs < CS; ++cs) {
-    const int col = c0 + min(16 * cs + n, ncols - 1);  // (columns without a query repeat the last one)
-    const int row = col / gq, head = kv * gq + col % gq, b = it.request + row / a.sq;
-    see[cs] = min(length_of(a, in.lens, b) - a.sq + 1 + row % a.sq, it.hi);
-    least = min(least, see[cs]);
-    const uint16_t* qp = in.q + (((size_t)it.request * a.sq + row) * a.Hq + head) * D;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-        if (!kQLds || wave == (cs * C + c) % kWaves) {
-          const u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j);
-          if (kQLds)
-            s_q[64 * ((cs * C + c) * 2 + j) + lane] = x;
-          else
-            qf[cs][c][j] = x;
-        }
-  }
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
-  if (kQLds) __syncthreads();
-
-  f32x4 acc[CS][C][4] = {};
-  float m[CS], l[CS];
-#pragma unroll
-  for (int cs = 0; cs < CS; ++cs) m[cs] = -INFINITY, l[cs] = 0.0f;
-  int e_ref = 0, e_top = -1000;
-
-  // ---- page walk: the wave takes rows r0 + wave, + kWaves, ...  A row's registers
+  // ---- page walk: the wave takes rows r0 + wave, + kRowWaves, ...  A row's registers
   // are refilled with the next row, K's as soon as the scores are formed and V's after
   // the value products.  Page IDs are read one turn before the loads.
-  const int32_t* const table = in.tables + (size_t)it.request * a.max_pages;
+  const Table table = table_of(a, in, it);
   const uint32_t koff = n * D + 16 * g, voff = lane * 16;
   const int base = it.lo / kRow, last = base + r1 - 1;  // (rows past the end read the last one again)
-  auto page_of = [&](int r) { return uniform(table[min(r, last) * kRow / P]); };
+  auto page_of = [&](int r) { return table[min(r, last) * kRow / P]; };
   auto run_of = [&](int pid) {
     return (size_t)((uint32_t)pid < (uint32_t)a.num_pages ? pid : 0) * a.Hkv + kv;
   };
@@ -213,6 +430,48 @@ __device__ __forceinline__ void walk(const Args& a, const Cache& in, const Item&
       for (int c = 0; c < C; ++c)
         w.v[t][c] = *reinterpret_cast<const u32x4*>(vp + voff + t * 16 * D + c * 1024);
   };
+
+  Row<D> w;
+  int r = base + r0 + wave;
+  int pid = page_of(r), ahead = page_of(r + kRowWaves);
+  fetch_k(w, r, pid);
+  fetch_v(w, r, pid);
+
+  // ---- queries as B operands: column n of each set, dims 64 c + 16 g + 8 j .., in
+  // registers or, where they would fill them, in LDS
+  constexpr bool kQLds = CS > 1;
+  int see[CS], least = 0x7fffffff;  // positions the columns' queries see
+  u32x4 qf[CS][C][2];
+  u32x4* const s_q = reinterpret_cast<u32x4*>(smem);
+  __syncthreads();  // (LDS still holds what was before)
+#pragma unroll
+  for (int cs = 0; cs < CS; ++cs) {
+    const int col = c0 + min(16 * cs + n, ncols - 1);  // (columns without a query repeat the last one)
+    const uint16_t* const qp = query_of<D>(a, in, batch, it, col, kv, see[cs]);
+    least = min(least, see[cs]);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (!kQLds || wave == (cs * C + c) % kRowWaves) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j) ^ a.flip;
+          if (kQLds)
+            s_q[64 * ((cs * C + c) * 2 + j) + lane] = x;
+          else
+            qf[cs][c][j] = x;
+        }
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
+  int masked = least - kRow + 1;  // the first position at which a row is masked
+  asm("" : "+v"(masked));         // (in a vector register, as in the tiles' walk)
+  if (kQLds) __syncthreads();
+
+  f32x4 acc[CS][C][4] = {};
+  float m[CS], l[CS];
+#pragma unroll
+  for (int cs = 0; cs < CS; ++cs) m[cs] = -INFINITY, l[cs] = 0.0f;
+  int e_ref = 0, e_top = -1000;
 
   // scores of a row in log2 units, and the exponents of its values
   auto scores = [&](const Row<D>& w, int r, float (&s)[CS][2][4], int (&ev)[2]) {
@@ -244,7 +503,7 @@ __device__ __forceinline__ void walk(const Args& a, const Cache& in, const Item&
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[cs][t][i] = x[t][cs][i] * f;
     }
-    if (pos0 + kRow > least || pos0 < it.lo) {
+    if (pos0 >= masked || pos0 < it.lo) {
       // positions that a query does not see, slots not written yet, and slots before
       // the item's (their codes, a NaN among them, and exponents are not looked at)
 #pragma unroll
@@ -352,23 +611,16 @@ __device__ __forceinline__ void walk(const Args& a, const Cache& in, const Item&
     }
   };
 
-  {
-    Row<D> w;
-    int r = base + r0 + wave;
-    int pid = page_of(r), ahead = page_of(r + kWaves);
-    fetch_k(w, r, pid);
-    fetch_v(w, r, pid);
-    for (; r <= last; r += kWaves) {
-      const bool on = (uint32_t)pid < (uint32_t)a.num_pages;
-      float s[CS][2][4];
-      int ev[2];
-      scores(w, r, s, ev);
-      fetch_k(w, r + kWaves, ahead);
-      if (on) attend(w, r, s, ev);
-      fetch_v(w, r + kWaves, ahead);
-      pid = ahead;
-      ahead = page_of(r + 2 * kWaves);
-    }
+  for (; r <= last; r += kRowWaves) {
+    const bool on = (uint32_t)pid < (uint32_t)a.num_pages;
+    float s[CS][2][4];
+    int ev[2];
+    scores(w, r, s, ev);
+    fetch_k(w, r + kRowWaves, ahead);
+    if (on) attend(w, r, s, ev);
+    fetch_v(w, r + kRowWaves, ahead);
+    pid = ahead;
+    ahead = page_of(r + 2 * kRowWaves);
   }
 
   // ---- merge the waves in LDS, one set of columns after the other: o (units 1), m, l
@@ -390,18 +642,18 @@ __device__ __forceinline__ void walk(const Args& a, const Cache& in, const Item&
       if (g == 0) mine[D] = m[cs], mine[D + 1] = den;
     }
     __syncthreads();
-    for (int i = tid; i < here * (D / 4); i += kThreads) {
+    for (int i = tid; i < here * (D / 4); i += kRowThreads) {
       const int at = i / (D / 4), d4 = i % (D / 4);
       const float* const part = smem + at * kPart;
-      float mw[kWaves], M = -INFINITY, sum = 0.0f;
+      float mw[kRowWaves], M = -INFINITY, sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < kRowWaves; ++w) {
         mw[w] = part[w * wide + D];
         M = fmaxf(M, mw[w]);
       }
       f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
+      for (int w = 0; w < kRowWaves; ++w) {
         const float f = mw[w] == -INFINITY ? 0.0f : exp2_(mw[w] - M);
         num += *reinterpret_cast<const f32x4*>(part + w * wide + 4 * d4) * f;
         sum = fmaf(f, part[w * wide + D + 1], sum);
@@ -413,109 +665,107 @@ __device__ __forceinline__ void walk(const Args& a, const Cache& in, const Item&
   }
 }
 
+// The same by tiles.
+template <int D, bool BF16, int NC>
+__device__ __forceinline__ void walk_columns(const Args& a, const Cache& in, const Batch& batch,
+                                             const Item& it, int c0,
+                                             int kv, int j0, int j1, float* rec, float* smem) {
+  constexpr int C = D / 64;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const int wave = uniform(tid >> 6);
+  const int wcol = c0 + wave * 16 * NC;
+  const bool active = wcol < it.cols;
+  int see[NC], least = 0x7fffffff;
+  u32x4 qf[NC][C][2];
+  __syncthreads();  // (LDS still holds what was before)
+#pragma unroll
+  for (int cs = 0; cs < NC; ++cs) {  // (columns past the end repeat the last)
+    const uint16_t* const qp = query_of<D>(a, in, batch, it, min(wcol + 16 * cs + n, it.cols - 1), kv, see[cs]);
+    least = min(least, see[cs]);
+    tiles::load_q<C, BF16>(qf[cs], qp, g, a.flip);
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
+  f32x4 acc[NC][C][4] = {};
+  float m[NC], l[NC];
+#pragma unroll
+  for (int cs = 0; cs < NC; ++cs) m[cs] = -INFINITY, l[cs] = 0.0f;
+  int e_ref = 0, e_top = -1000;
+  // (the first position at which a tile is masked, in a vector register: with a scalar
+  // branch around the masks the compiler holds more at once, and spills)
+  int masked = least - kTile + 1;
+  asm("" : "+v"(masked));
+  const struct {
+    int masked;
+    const int (&see)[NC];
+    __device__ __forceinline__ bool hides_some(int pos0) const { return pos0 >= masked; }
+    __device__ __forceinline__ bool hides(int cs, int pos) const { return pos >= see[cs]; }
+  } sees{masked, see};
+  u32x4(*const lds)[8 * D] = reinterpret_cast<u32x4(*)[8 * D]>(smem);
+  walk_tiles<D, BF16, NC>(in.k_codes, in.k_exps, in.v_codes, in.v_exps,
+                          tid, table_of(a, in, it), a.Hkv, kv, a.P, a.block_shift, a.num_pages,
+                          it.hi, j0, j1, a.scale_log2, qf, sees, active, lds, lds + 2,
+                          acc, m, l, e_ref, e_top);
+  if (!active) return;
+  const float unit = __builtin_ldexpf(1.0f, e_ref);
+#pragma unroll
+  for (int cs = 0; cs < NC; ++cs) {
+    const float den = col_sum(l[cs]);
+    const int at = wave * 16 * NC + 16 * cs + n;
+    if (c0 + at >= it.cols) continue;
+    float* const to = rec + (size_t)at * (D + 4);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(to + 64 * c + 16 * g + 4 * i) =
+            f32x4{acc[cs][c][0][i], acc[cs][c][1][i], acc[cs][c][2][i], acc[cs][c][3][i]} * unit;
+    if (g == 0) *reinterpret_cast<f32x2*>(to + D) = f32x2{m[cs], den};
+  }
+}
+
 template <int D, bool BF16>
-__global__ __launch_bounds__(kThreads) void kv8_shared_kernel(
+__global__ __launch_bounds__(kRowThreads, kRowBlocks) void kv8_shared_rows_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
     const uint16_t* __restrict__ q, const int32_t* __restrict__ tables,
     const int32_t* __restrict__ lens, float* __restrict__ recs, const Args a) {
-  extern __shared__ __align__(16) float smem[];
-  __shared__ int64_t s_wave[kWaves], s_upto[kThreads + 1], s_start;
-  __shared__ int s_item;
-  __shared__ int32_t s_first[kGroupsLds + 1], s_shared[kGroupsLds];
-  const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables, lens};
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-
-  // ---- the groups
-  Groups gr{a.first, a.shared, a.G, true};
-  int bad = 0;
-  for (int i = tid; i <= a.G; i += kThreads) {
-    const int at = a.first[i];
-    bad |= i == 0 ? at != 0 : at < a.first[i - 1];
-    if (i == a.G) bad |= at != a.B;
-    if (a.G <= kGroupsLds) {
-      s_first[i] = at;
-      if (i < a.G) s_shared[i] = a.shared[i];
-    }
+  extern __shared__ __align__(1024) float smem[];
+  __shared__ Plan<kRowThreads> plan;
+  const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables};
+  if (!plan.begin<D, false>(a, lens)) return;
+  while (plan.next<D, false>(lens)) {
+    const Args f = plan.args();
+    const Segment t = plan.part();
+    const Batch batch = plan.batch(f, lens, plan.state.valid);
+    if (t.it.kind == kRows1)
+      walk_rows<D, BF16, 1>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+    else
+      walk_rows<D, BF16, 2>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
   }
-  gr.valid = !__syncthreads_or(bad);
-  if (a.G <= kGroupsLds) gr.first = s_first, gr.shared = s_shared;
+}
 
-  // ---- the line: work of all items, and of the first window of them
-  const int items = a.G + a.B;
-  int64_t mine = 0, total = 0;
-  for (int i = tid; i < items; i += kThreads) {
-    const int64_t x = work_of(a, item_of<D>(a, lens, gr, i));
-    if (i < kThreads) mine = x;
-    total += x;
-  }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
-  if (lane == 0) s_wave[wave] = total;
-  __syncthreads();
-  total = 0;
-  for (int w = 0; w < kWaves; ++w) total += s_wave[w];
-  total = uniform(total);
-  const int64_t piece = max((total + gridDim.x - 1) / gridDim.x, (int64_t)(row_cost(1) * kWaves * kMinRows));
-  const int64_t begin = blockIdx.x * piece, end = min(begin + piece, total);
-
-  int window = 0;     // its first item
-  int64_t carry = 0;  // the line before it
-  // s_upto[i + 1]: the line up to the window's item i, itself among it
-  auto scan = [&]() {
-    int64_t sum = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t up = __shfl_up(sum, o);
-      if (lane >= o) sum += up;
-    }
-    __syncthreads();
-    if (lane == 63) s_wave[wave] = sum;
-    __syncthreads();
-    sum += carry;
-    for (int w = 0; w < wave; ++w) sum += s_wave[w];
-    s_upto[tid + 1] = sum;
-    if (tid == 0) s_upto[0] = carry;
-    __syncthreads();
-  };
-  if (begin < end) scan();
-  for (int64_t x = begin; x < end;) {
-    // ---- the item at x
-    while (x >= uniform(s_upto[kThreads])) {
-      carry = uniform(s_upto[kThreads]), window += kThreads;
-      mine = window + tid < items ? work_of(a, item_of<D>(a, lens, gr, window + tid)) : 0;
-      scan();
-    }
-    __syncthreads();
-    if (x < s_upto[tid + 1] && x >= s_upto[tid]) s_item = window + tid, s_start = s_upto[tid];
-    __syncthreads();
-    const int64_t start = uniform(s_start);
-    const int item = uniform(s_item);
-    Item it = item_of<D>(a, lens, gr, item);
-    it.request = uniform(it.request), it.requests = uniform(it.requests);
-    it.lo = uniform(it.lo), it.hi = uniform(it.hi), it.rows = uniform(it.rows);
-    it.sets = uniform(it.sets), it.chunks = uniform(it.chunks), it.unit = uniform(it.unit);
-    const int cost = row_cost(it.sets), span = it.rows * cost;
-    const int u = (int)((x - start) / span);
-    const int64_t at = start + (int64_t)u * span;
-    const int r0 = (int)((x - at + cost - 1) / cost);
-    const int r1 = (int)min((int64_t)it.rows, (end - at + cost - 1) / cost);
-    const int kv = u % a.Hkv, chunk = u / a.Hkv;
-    const bool own = item >= a.G;
-    const int unit = it.unit + u, id = own ? unit - a.group_units : unit;
-    if (r0 == 0 && tid == 0) {
-      const int from = (int)(at / piece), to = (int)((at + span - cost) / piece);
-      a.info[unit] = make_int2(id + from, to - from + 1);
-    }
-    if (r0 < r1) {
-      float* const rec = recs + (own ? a.own_recs + ((int64_t)id + blockIdx.x) * (a.own_cols * (D + 4))
-                                     : ((int64_t)id + blockIdx.x) * (16 * max_sets<D>() * (D + 4)));
-      if (it.sets == 1)
-        walk<D, BF16, 1>(a, in, it, chunk, kv, r0, r1, rec, smem);
-      else
-        walk<D, BF16, 2>(a, in, it, chunk, kv, r0, r1, rec, smem);
-    }
-    x = at + span;
+template <int D, bool BF16>
+__global__ __launch_bounds__(kTileThreads) void kv8_shared_tiles_kernel(
+    const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
+    const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
+    const uint16_t* __restrict__ q, const int32_t* __restrict__ tables,
+    const int32_t* __restrict__ lens, float* __restrict__ recs, const Args a) {
+  extern __shared__ __align__(1024) float smem[];
+  __shared__ Plan<kTileThreads> plan;
+  const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables};
+  if (!plan.begin<D, true>(a, lens)) return;
+  while (plan.next<D, true>(lens)) {
+    const Args f = plan.args();
+    const Segment t = plan.part();
+    const Batch batch = plan.batch(f, lens, plan.state.valid);
+    constexpr int kMost = widest(D) / 128;
+    if (kMost == 1 || t.it.kind == kTiles1)
+      walk_columns<D, BF16, 1>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+    else
+      walk_columns<D, BF16, kMost>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
   }
 }
 
@@ -525,23 +775,23 @@ constexpr int kJoinWaves = 4;
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
     const float* __restrict__ recs, const int32_t* __restrict__ lens, uint16_t* __restrict__ out,
-    float* __restrict__ lse, const Args a, int blocks) {
+    float* __restrict__ lse, const Args a, int tile_blocks, int row_blocks) {
   constexpr int kPart = D + 4, kAt = 4;
   __shared__ f32x4 s_num[kJoinWaves][64];
   __shared__ f32x2 s_ml[kJoinWaves][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int kv = blockIdx.y, b = blockIdx.z, gq = a.Hq / a.Hkv, pairs = gq * a.sq;
+  const int kv = blockIdx.y, b = blockIdx.z, gq = a.gq, pairs = gq * a.sq;
 
+  Batch batch{a.first, a.shared, lens, nullptr, nullptr, nullptr, a.G, a.max_pages * a.P, false, true};
   int bad = 0;
   for (int i = tid; i <= a.G; i += 64 * kJoinWaves) {
     const int at = a.first[i];
     bad |= i == 0 ? at != 0 : at < a.first[i - 1];
     if (i == a.G) bad |= at != a.B;
   }
-  Groups gr{a.first, a.shared, a.G, true};
-  gr.valid = !__syncthreads_or(bad);
-  const int group = gr.valid ? gr.of(b) : 0;
-  const int shared = gr.valid ? shared_of(a, lens, gr, group) : 0, len = length_of(a, lens, b);
+  batch.valid = !__syncthreads_or(bad);
+  const int group = batch.valid ? batch.of(b) : 0;
+  const int shared = batch.valid ? batch.shared(group) : 0, len = batch.length(b);
 
   const int i = blockIdx.x * 64 + lane, pair = min(i / (D / 4), pairs - 1), d4 = i % (D / 4);
   f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -570,20 +820,26 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
       M = mx;
     }
   };
+  int id, at, entry;
   if (shared > 0) {
-    const int from = gr.first[group], cols = (gr.first[group + 1] - from) * pairs;
-    const int width = 16 * sets_for(D, cols), col = (b - from) * pairs + pair;
-    const int unit = (from * pairs / (16 * max_sets<D>()) + group + col / width) * a.Hkv + kv;
-    const int2 in = a.info[unit];
-    const int64_t stride = (int64_t)(16 * max_sets<D>()) * kPart;
-    add(recs + in.x * stride + (int64_t)(col % width) * kPart, stride, min(in.y, blocks));
+    constexpr int W = widest(D);
+    const int from = batch.first(group), cols = (batch.first(group + 1) - from) * pairs;
+    const int col = (b - from) * pairs + pair, full = cols & -W, in_full = col < full;
+    const int kind = kind_of(D, in_full ? W : cols - full);
+    const int off = (col - (in_full ? 0 : full)) & (width_of(kind) - 1);  // in its chunk
+    group_place<D>(a, from, group, col - off, kv, id, at, entry);
+    const int2 in = a.info[entry];
+    const bool by_tiles = kind >= kTiles1;
+    const int64_t stride = (int64_t)(by_tiles ? W : kRowCols) * kPart;
+    add(recs + (by_tiles ? 0 : a.row_recs) + in.x * stride + (int64_t)((by_tiles ? at : at % kRowCols) + off) * kPart,
+        stride, min(in.y, by_tiles ? tile_blocks : row_blocks));
   }
   if (len > shared) {
-    const int width = 16 * sets_for(D, a.own_cols);
-    const int unit = (b * a.chunks + pair / width) * a.Hkv + kv;
-    const int2 in = a.info[a.group_units + unit];
+    const int width = width_of(a.own_kind);
+    own_place<D>(a, b, pair / width, kv, id, entry);
+    const int2 in = a.info[entry];
     const int64_t stride = (int64_t)a.own_cols * kPart;
-    add(recs + a.own_recs + in.x * stride + (int64_t)(pair % width) * kPart, stride, min(in.y, blocks));
+    add(recs + a.own_recs + in.x * stride + (int64_t)(pair % width) * kPart, stride, min(in.y, row_blocks));
   }
   s_num[wave][lane] = num;
   s_ml[wave][lane] = f32x2{M, den};
@@ -608,51 +864,62 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
 }
 
 // How the workspace is laid out.
-struct Plan {
-  int blocks, group_units, chunks, own_cols;
-  int64_t own_recs;
+struct Layout {
+  int tile_blocks, row_blocks, group_units, own_kind, chunks, own_cols;
+  int64_t row_recs, own_recs;
   size_t recs, bytes;
 };
-Plan plan_of(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq) {
-  const int D = L.head_dim, Hkv = L.num_kv_heads, pairs = Hq / Hkv * sq;
-  const int sets = 2, width = 16 * sets_for(D, pairs);
-  Plan p;
-  p.blocks = num_cus();
-  p.group_units = (int)(((int64_t)B * pairs / (16 * sets) + G + 1) * Hkv);
+Layout layout_of(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq) {
+  const int D = L.head_dim, Hkv = L.num_kv_heads, pairs = Hq / Hkv * sq, W = widest(D);
+  Layout p;
+  p.tile_blocks = (int64_t)B * pairs > kRowCols ? num_cus() : 0;  // (else no group has so many columns)
+  p.row_blocks = kRowBlocks * num_cus();
+  p.group_units = (int)(((int64_t)B * pairs / W + G + 1) * Hkv);
+  p.own_kind = pairs <= 16 ? kRows1 : kRows2;
+  const int width = width_of(p.own_kind);
   p.own_cols = std::min(pairs, width);
   p.chunks = (pairs + width - 1) / width;
   const int64_t own_units = (int64_t)B * p.chunks * Hkv;
-  p.own_recs = ((int64_t)p.group_units + p.blocks) * (16 * sets) * (D + 4);
-  p.recs = ((size_t)(p.group_units + own_units) * sizeof(int2) + 15) / 16 * 16;
-  p.bytes = p.recs + (size_t)(p.own_recs + (own_units + p.blocks) * p.own_cols * (D + 4)) * sizeof(float);
+  p.row_recs = p.tile_blocks ? ((int64_t)p.group_units + p.tile_blocks) * W * (D + 4) : 0;
+  p.own_recs = p.row_recs + ((int64_t)p.group_units + p.row_blocks) * kRowCols * (D + 4);
+  p.recs = ((size_t)((int64_t)p.group_units * (W / kSub) + own_units) * sizeof(int2) + 15) / 16 * 16;
+  p.bytes = p.recs + (size_t)(p.own_recs + (own_units + p.row_blocks) * p.own_cols * (D + 4)) * sizeof(float);
   return p;
 }
 
 template <int D, bool BF16>
-hipError_t launch_t(const Cache& in, const Args& a, const Plan& p, float* recs, void* out, float* lse,
-                    hipStream_t stream) {
-  const auto kernel = kv8_shared_kernel<D, BF16>;
-  const size_t lds = std::max<size_t>(sizeof(float) * kWaves * 16 * (D + 4), 16 * max_sets<D>() * D * 2);
-  if (lds > 49152) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+hipError_t launch_t(const Cache& in, const int32_t* lens, const Args& a, const Layout& p, float* recs,
+                    void* out, float* lse, hipStream_t stream) {
+  auto go = [&](auto kernel, int blocks, int threads, size_t lds) {
+    if (lds > 32768) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), lds, stream, in.k_codes, in.k_exps,
+                       in.v_codes, in.v_exps, in.q, in.tables, lens, recs, a);
+    return hipGetLastError();
+  };
+  if (p.tile_blocks) {
+    const hipError_t e = go(kv8_shared_tiles_kernel<D, BF16>, p.tile_blocks, kTileThreads,
+                            4 * 8 * D * sizeof(u32x4));
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(kernel, dim3(p.blocks), dim3(kThreads), lds, stream, in.k_codes, in.k_exps,
-                     in.v_codes, in.v_exps, in.q, in.tables, in.lens, recs, a);
-  const hipError_t e = hipGetLastError();
+  // (the waves' merge; the queries before it take less)
+  const hipError_t e = go(kv8_shared_rows_kernel<D, BF16>, p.row_blocks, kRowThreads,
+                          sizeof(float) * kRowWaves * 16 * (D + 4));
   if (e != hipSuccess) return e;
-  const int runs = a.Hq / a.Hkv * a.sq * (D / 4);
+  const int runs = a.gq * a.sq * (D / 4);
   hipLaunchKernelGGL((kv8_shared_join_kernel<D, BF16>), dim3((runs + 63) / 64, a.Hkv, a.B),
-                     dim3(64 * kJoinWaves), 0, stream, recs, in.lens, static_cast<uint16_t*>(out), lse,
-                     a, p.blocks);
+                     dim3(64 * kJoinWaves), 0, stream, recs, lens, static_cast<uint16_t*>(out), lse,
+                     a, p.tile_blocks, p.row_blocks);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t kv8_shared_bytes(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq) {
-  return plan_of(L, B, G, sq, Hq).bytes;
+  return layout_of(L, B, G, sq, Hq).bytes;
 }
 
 hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
@@ -661,20 +928,21 @@ hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
                              const int32_t* group_start, const int32_t* shared_lens, int32_t G,
                              float softmax_scale, void* ws, void* out, float* lse,
                              hipStream_t stream) {
-  const Plan p = plan_of(L, B, G, sq, Hq);
+  const Layout p = layout_of(L, B, G, sq, Hq);
   int shift = 0;
   while ((1 << shift) < L.group_size) ++shift;
   const Cache in{static_cast<const uint8_t*>(pool.k_codes), static_cast<const uint8_t*>(pool.k_meta),
                  static_cast<const uint8_t*>(pool.v_codes), static_cast<const uint8_t*>(pool.v_meta),
-                 static_cast<const uint16_t*>(q), block_tables, seq_lens};
+                 static_cast<const uint16_t*>(q), block_tables};
   Args a{};
   a.first = group_start, a.shared = shared_lens, a.info = static_cast<int2*>(ws);
-  a.B = B, a.G = G, a.sq = sq, a.Hq = Hq, a.Hkv = L.num_kv_heads, a.P = L.page_size;
+  a.B = B, a.G = G, a.sq = sq, a.Hq = Hq, a.Hkv = L.num_kv_heads, a.gq = Hq / L.num_kv_heads, a.P = L.page_size;
   a.block_shift = shift, a.num_pages = L.num_pages, a.max_pages = max_pages;
-  a.group_units = p.group_units, a.chunks = p.chunks, a.own_cols = p.own_cols, a.own_recs = p.own_recs;
-  a.scale_log2 = softmax_scale * 1.44269504088896340736f;
+  a.group_units = p.group_units, a.own_kind = p.own_kind, a.chunks = p.chunks, a.own_cols = p.own_cols, a.row_recs = p.row_recs, a.own_recs = p.own_recs;
+  a.scale_log2 = std::fabs(softmax_scale) * tiles::kLog2e;
+  a.flip = softmax_scale < 0.0f ? 0x80008000u : 0u;
   float* const recs = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.recs);
-  auto go = [&](auto fn) { return fn(in, a, p, recs, out, lse, stream); };
+  auto go = [&](auto fn) { return fn(in, seq_lens, a, p, recs, out, lse, stream); };
   if (L.head_dim == 64) return bf16 ? go(launch_t<64, true>) : go(launch_t<64, false>);
   if (L.head_dim == 128) return bf16 ? go(launch_t<128, true>) : go(launch_t<128, false>);
   return bf16 ? go(launch_t<256, true>) : go(launch_t<256, false>);
