@@ -93,9 +93,10 @@ __device__ __forceinline__ int64_t whole(int64_t y, int64_t d) {
 
 // Groups and lengths, from LDS where they fit.  The groups are valid only if their
 // bounds ascend from 0 to B.
+typedef const __attribute__((address_space(3))) int32_t* Lds;
 struct Batch {
   const int32_t *g_first, *g_shared, *g_lens;
-  const int32_t *s_first, *s_shared, *s_lens;
+  Lds s_first, s_shared, s_lens;
   int groups, cap;
   bool in_lds, valid;
   __device__ __forceinline__ int first(int g) const { return in_lds ? s_first[g] : g_first[g]; }
@@ -161,18 +162,6 @@ __device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i
   return t;
 }
 
-// How the line is cut.  Where units are few, each begins a piece of its own and its
-// length is rounded up to whole pieces, so that no block starts twice; else units
-// follow one another, each with its start's cost.
-struct Line {
-  int64_t piece;
-  bool apart;
-  __device__ __forceinline__ int64_t span(const Item& t) const {
-    const int64_t work = t.work();
-    if (!work) return 0;
-    return apart ? (whole(work - 1, piece) + 1) * piece : start_of(t.kind) + work;
-  }
-};
 // A chunk's record slot, its first column there, and its entry of `info`, for a KV head:
 // of a group's columns from `col` on, the group's first request and number given, ..
 template <int D>
@@ -192,9 +181,9 @@ __device__ __forceinline__ void own_place(const Args& a, int request, int chunk,
 // Where a block is on the line: at x, up to end; the window of items that is summed up
 // begins with item `window`.
 struct State {
-  int64_t x, end;
+  int64_t x, end, piece;
   int window;
-  bool valid;
+  bool valid, apart;
 };
 // Steps r0 .. r1 - 1 of a unit: its chunk's first column, KV head and record.
 struct Segment {
@@ -202,29 +191,41 @@ struct Segment {
   int col, kv, r0, r1;
   int64_t rec;
 };
-// The plan of a block of T threads.  (What lives from one segment to the next is in LDS,
-// so that the walks have the registers.)
+// The plan of a block of T threads: which segments it has.  Where units are few, each is
+// cut into equal shares, as many for all units as there are blocks, and a block has one
+// share; else the units follow one another on a line, each with its start's cost, and
+// the line is cut into pieces of one length.  (What lives from one segment to the next
+// is in LDS, so that the walks have the registers.)
 template <int T>
 struct Plan {
+  static constexpr int kTeams = T / 64;
   Args a;
-  Line line;
   State state;
   Segment segment;
   int64_t upto[T + 1];  // the line up to the window's item i, itself among it: upto[i + 1]
   Item items[T];
-  int64_t sum[T / 64];
-  int units[T / 64], starts[T / 64];
+  int64_t sum[kTeams];
+  int units[kTeams], starts[kTeams];
   int32_t first[T + 1], shared[T], lens[2 * T];
 
   __device__ __forceinline__ Batch batch(const Args& g, const int32_t* g_lens, bool valid) const {
-    return Batch{g.first, g.shared, g_lens, first, shared, lens, g.G, g.max_pages * g.P,
+    return Batch{g.first, g.shared, g_lens, (Lds)first, (Lds)shared, (Lds)lens, g.G, g.max_pages * g.P,
                  g.G <= T && g.B <= 2 * T, valid};
   }
+  // An item's part of the line.
+  static __device__ __forceinline__ int64_t span(const Item& t) {
+    const int64_t work = t.work();
+    return work ? start_of(t.kind) + work : 0;
+  }
+  // Shares of a unit's work (below 2^31) of at most `most` each.
+  static __device__ __forceinline__ int shares(int work, float most) {
+    return work ? max((int)ceilf((float)work / most), 1) : 0;
+  }
 
-  // All threads; false: nothing for this block.
+  // All threads: the block's first segment; false: there is none.
   template <int D, bool TILES>
   __device__ __forceinline__ bool begin(const Args& g, const int32_t* g_lens) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), blocks = gridDim.x;
+    const int tid = threadIdx.x, lane = tid & 63, team = uniform(tid >> 6), blocks = gridDim.x;
     Batch b = batch(g, g_lens, true);
     int bad = 0;
     for (int i = tid; i <= g.G; i += T) {
@@ -240,47 +241,115 @@ struct Plan {
       for (int i = tid; i < g.B; i += T) lens[i] = g_lens[i];
     b.valid = !__syncthreads_or(bad);
 
+    // all items' work, units and starts
     const int n = TILES ? 2 * g.G : 2 * g.G + g.B;
     int64_t work = 0;
-    int count = 0, begins = 0;
+    int count = 0, begins = 0, units_here = 0, work_here = 0;
+    Item t = {};
     for (int i = tid; i < n; i += T) {
-      const Item t = item_of<D, TILES>(g, b, i);
+      t = item_of<D, TILES>(g, b, i);
       const int64_t w = t.work();
       const int m = w ? t.chunks() * g.Hkv : 0;
       work += w * m, count += m, begins += m * start_of(t.kind);
+      work_here = (int)min(w, (int64_t)0x7fffffff), units_here = m;
       items[tid] = t;
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1)
       work += __shfl_xor(work, o), count += __shfl_xor(count, o), begins += __shfl_xor(begins, o);
-    if (lane == 0) sum[wave] = work, units[wave] = count, starts[wave] = begins;
+    if (lane == 0) sum[team] = work, units[team] = count, starts[team] = begins;
     __syncthreads();
     work = 0, count = begins = 0;
 #pragma unroll
-    for (int w = 0; w < T / 64; ++w) work += sum[w], count += units[w], begins += starts[w];
+    for (int w = 0; w < kTeams; ++w) work += sum[w], count += units[w], begins += starts[w];
     work = uniform(work), count = uniform(count), begins = uniform(begins);
-    constexpr int64_t kLeast = TILES ? 2 * cost_of(kTiles1) : cost_of(kRows1) * kRowWaves * kMinRows;
-    Line l;
-    l.apart = 2 * count <= blocks;
-    l.piece = max(l.apart ? whole(work, blocks - count) + 1 : whole(work + begins, blocks) + 1, kLeast);
-    const int64_t from = blockIdx.x * l.piece;
-    // (no more than this is behind: the line's own end is known with its last item)
-    if (from >= (l.apart ? work + count * l.piece : work + begins)) return false;
-    if (tid == 0) {
-      a = g, line = l;
-      state = State{from, from + l.piece, -T, b.valid};
-      upto[T] = 0;  // (no window yet)
+    if (count == 0) return false;
+    constexpr int kLeast = TILES ? 2 * cost_of(kTiles1) : cost_of(kRows1) * kRowWaves * kMinRows;
+    if (2 * count > blocks || n > T || work >= 0x40000000) {  // the line
+      if (tid == 0) {
+        a = g;
+        const int64_t piece = max(whole(work + begins, blocks) + 1, (int64_t)kLeast);
+        const int64_t from = blockIdx.x * piece;
+        state = State{from, min(from + piece, work + begins), piece, -T, b.valid, false};
+        upto[T] = 0;  // (no window yet)
+      }
+      __syncthreads();
+      return next<D, TILES>(g_lens);
+    }
+
+    // Shares: as many as there are blocks, or less.  Their length lies between work /
+    // blocks and work / (blocks - count); each wave counts those of one length, the
+    // least that are not too many are taken.
+    const float low = (float)work / (float)blocks, high = (float)work / (float)(blocks - count) * 1.0001f + 1.0f;
+    auto length = [&](int w) { return fmaxf(low + (high - low) * ((float)w / (kTeams - 1)), (float)kLeast); };
+    __syncthreads();  // (`units` is written again)
+    int many = 0;
+    for (int i = lane; i < n; i += 64) {
+      const Item u = items[i];
+      const int w = (int)u.work();
+      if (w) many += shares(w, length(team)) * (u.chunks() * g.Hkv);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) many += __shfl_xor(many, o);
+    if (lane == 0) units[team] = many;
+    __syncthreads();
+    int pick = kTeams - 1;
+#pragma unroll
+    for (int w = kTeams - 2; w >= 0; --w)
+      if (units[w] <= blocks) pick = w;
+    // the block's share: one thread's item has it
+    const int each = shares(work_here, length(pick)), all = each * units_here;
+    int to = all;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int up = __shfl_up(to, o);
+      if (lane >= o) to += up;
+    }
+    if (lane == 63) starts[team] = to;
+    if (tid == 0) a = g, state.apart = true, state.valid = b.valid, segment.r0 = segment.r1 = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kTeams; ++w) to += w < team ? starts[w] : 0;
+    const int j = (int)blockIdx.x - (to - all);
+    if (j >= 0 && j < all) {
+      const int u = (int)(((float)j + 0.5f) / (float)each), share = j - u * each;  // (both below 2^16)
+      const uint32_t steps = t.steps(), size = (steps + each - 1) / (uint32_t)each;
+      const int r0 = (int)min(share * size, steps), r1 = (int)min(r0 + size, steps);
+      put<D, TILES>(g, t, tid, u, r0, r1, (int)((steps + size - 1) / size));
     }
     __syncthreads();
-    return true;
+    return uniform(segment.r0) < uniform(segment.r1);
+  }
+
+  // Steps r0 .. r1 - 1 of unit u of item i, which leaves `records` records, the first of
+  // them by the block that has its first step.
+  template <int D, bool TILES>
+  __device__ __forceinline__ void put(const Args& g, const Item& it, int i, int u, int r0, int r1,
+                                      int records) {
+    const int chunk = (int)(((float)u + 0.5f) / (float)g.Hkv), kv = u - chunk * g.Hkv;  // (u below 2^17)
+    const int col = it.col0 + (chunk << width_log2(it.kind));
+    int id, first_col, entry;
+    int64_t rec;
+    if (TILES || i < 2 * g.G) {
+      group_place<D>(g, it.request, i >> 1, col, kv, id, first_col, entry);
+      const int64_t slot = (int64_t)id + blockIdx.x;
+      rec = TILES ? (slot * widest(D) + first_col) * (D + 4)
+                  : g.row_recs + (slot * kRowCols + first_col % kRowCols) * (D + 4);
+    } else {
+      own_place<D>(g, it.request, chunk, kv, id, entry);
+      rec = g.own_recs + ((int64_t)id + blockIdx.x) * (g.own_cols * (D + 4));
+    }
+    if (r0 == 0 && r1 > 0) g.info[entry] = make_int2(id + blockIdx.x, records);
+    segment = Segment{it, col, kv, r0, r1, rec};
   }
 
   // All threads: the block's next segment; false: none is left.
   template <int D, bool TILES>
   __device__ __forceinline__ bool next(const int32_t* g_lens) {
+    if (uniform((int)state.apart)) return false;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
-    const int lane = tid & 63, wave = uniform(tid >> 6);
+    const int lane = tid & 63, team = uniform(tid >> 6);
     const int n = uniform(TILES ? 2 * a.G : 2 * a.G + a.B);
     for (;;) {
       const int64_t x = uniform(state.x);
@@ -292,21 +361,17 @@ struct Plan {
         if (window >= n) return false;
         const bool mine = window + tid < n;
         if (n > T && mine) items[tid] = item_of<D, TILES>(a, batch(a, g_lens, state.valid), window + tid);
-        int64_t to = 0;
-        if (mine) {
-          const Item t = items[tid];
-          to = line.span(t) * (t.chunks() * a.Hkv);
-        }
+        int64_t to = mine ? span(items[tid]) * (items[tid].chunks() * a.Hkv) : 0;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
           const int64_t up = __shfl_up(to, o);
           if (lane >= o) to += up;
         }
-        if (lane == 63) sum[wave] = to;
+        if (lane == 63) sum[team] = to;
         __syncthreads();
         to += carry;
 #pragma unroll
-        for (int w = 0; w < T / 64; ++w) to += w < wave ? sum[w] : 0;
+        for (int w = 0; w < kTeams; ++w) to += w < team ? sum[w] : 0;
         upto[tid + 1] = to;
         if (tid == 0) upto[0] = carry, state.window = window;
         __syncthreads();
@@ -315,31 +380,16 @@ struct Plan {
       if (x >= upto[tid] && x < upto[tid + 1]) {  // one thread's item
         // the unit, and its steps that begin in the block's piece
         const Item it = items[tid];
-        const Line l = line;
         const int cost = cost_of(it.kind), steps = it.steps();
-        const int64_t span = l.span(it), end = state.end;
-        const int u = (int)whole(x - upto[tid], span);
-        const int64_t start = upto[tid] + u * span, at = start + (l.apart ? 0 : start_of(it.kind));
+        const int64_t length = span(it), end = state.end, in = x - upto[tid], piece = state.piece;
+        const int u = in < length ? 0 : (int)whole(in, length);
+        const int64_t start = x - in + u * length, at = start + start_of(it.kind), work = it.work();
         const int r0 = (int)whole(max(x - at, (int64_t)0) + cost - 1, cost);
-        const int r1 = min(steps, (int)whole(max(end - at, (int64_t)0) + cost - 1, cost));
-        const int chunk = (int)((uint32_t)u / (uint32_t)a.Hkv), kv = u - chunk * a.Hkv;
-        const int i = window + tid, col = it.col0 + (chunk << width_log2(it.kind));
-        int id, first_col, entry;
-        int64_t rec;
-        if (TILES || i < 2 * a.G) {
-          group_place<D>(a, it.request, i >> 1, col, kv, id, first_col, entry);
-          const int64_t slot = (int64_t)id + blockIdx.x;
-          rec = (TILES ? slot * widest(D) + first_col : a.row_recs / (D + 4) + slot * kRowCols + first_col % kRowCols) * (D + 4);
-        } else {
-          own_place<D>(a, it.request, chunk, kv, id, entry);
-          rec = a.own_recs + ((int64_t)id + blockIdx.x) * (a.own_cols * (D + 4));
-        }
-        if (r0 == 0 && r1 > 0) {
-          const int from = (int)whole(at, l.piece), to = (int)whole(at + it.work() - cost, l.piece);
-          a.info[entry] = make_int2(id + from, to - from + 1);
-        }
-        segment = Segment{it, col, kv, r0, r1, rec};
-        state.x = start + span;
+        const int r1 = end >= at + work ? steps : (int)whole(max(end - at, (int64_t)0) + cost - 1, cost);
+        // (the last step's piece, counted from this block's)
+        const int more = end >= at + work ? 0 : (int)whole(at + work - cost - (end - piece), piece);
+        put<D, TILES>(a, it, window + tid, u, r0, r1, 1 + more);
+        state.x = start + length;
       }
       __syncthreads();
       if (uniform(segment.r0) < uniform(segment.r1)) return true;  // (else a unit's start alone)
@@ -394,7 +444,8 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
   constexpr int C = D / 64;
   constexpr int kPart = D + 4;  // floats of a partial: o, m, l (16-byte rows)
   int tid = threadIdx.x;
-  asm volatile("" : "+v"(tid));
+  asm volatile("" : "+v"(tid));  // (opaque: what depends on it is not held from one segment to the next)
+  __builtin_assume(tid >= 0 && tid < kRowThreads);
   const int lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int P = a.P, ncols = min(16 * CS, it.cols - c0);
@@ -673,6 +724,7 @@ __device__ __forceinline__ void walk_columns(const Args& a, const Cache& in, con
   constexpr int C = D / 64;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));
+  __builtin_assume(tid >= 0 && tid < kTileThreads);
   const int lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = uniform(tid >> 6);
   const int wcol = c0 + wave * 16 * NC;
@@ -735,8 +787,7 @@ __global__ __launch_bounds__(kRowThreads, kRowBlocks) void kv8_shared_rows_kerne
   extern __shared__ __align__(1024) float smem[];
   __shared__ Plan<kRowThreads> plan;
   const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables};
-  if (!plan.begin<D, false>(a, lens)) return;
-  while (plan.next<D, false>(lens)) {
+  for (bool more = plan.begin<D, false>(a, lens); more; more = plan.next<D, false>(lens)) {
     const Args f = plan.args();
     const Segment t = plan.part();
     const Batch batch = plan.batch(f, lens, plan.state.valid);
@@ -756,8 +807,7 @@ __global__ __launch_bounds__(kTileThreads) void kv8_shared_tiles_kernel(
   extern __shared__ __align__(1024) float smem[];
   __shared__ Plan<kTileThreads> plan;
   const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables};
-  if (!plan.begin<D, true>(a, lens)) return;
-  while (plan.next<D, true>(lens)) {
+  for (bool more = plan.begin<D, true>(a, lens); more; more = plan.next<D, true>(lens)) {
     const Args f = plan.args();
     const Segment t = plan.part();
     const Batch batch = plan.batch(f, lens, plan.state.valid);
