@@ -17,7 +17,6 @@ namespace tiles {
 constexpr int kTile = 64;        // positions of a tile (in one page)
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kFar = 4;          // tiles by which lines are touched ahead of their fetch
 constexpr uint32_t kZeroExp = 1;  // the exponent byte of a block of zeros
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -43,11 +42,15 @@ __device__ __forceinline__ void walk_tiles(
     const uint8_t* v_codes, const uint8_t* v_exps,
     int tid, Table table, int Hkv, int kv, int P, int block_shift, int num_pages, int L,
     int j0, int j1, float scale_log2, const u32x4 (&qf)[NC][D / 64][2], const Sees& sees,
-    bool active, u32x4 (*tiles_k)[8 * D], u32x4 (*tiles_v)[8 * D],
+    bool active, u32x4* lds,
     f32x4 (&acc)[NC][D / 64][4], float (&m)[NC], float (&l)[NC], int& e_ref, int& e_top) {
-  constexpr int C = D / 64;
+  constexpr int C = D / 64, kTileSize = 8 * D;
   const int lane = tid & 63, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Two tiles of K and V each, in the order V1 K0 V0 K1: a turn's operands, V of one tile
+  // and K of the next, follow one another.
+  auto tile_k = [&](int j) JF_INLINE { return lds + (j & 1 ? 3 : 1) * kTileSize; };
+  auto tile_v = [&](int j) JF_INLINE { return lds + (j & 1 ? 0 : 2) * kTileSize; };
   // ---- tile transport: K's codes are fetched two tiles ahead and go to LDS one
   // tile ahead, V's one tile later each
   constexpr int kPieces = 4 * D / kThreads > 0 ? 4 * D / kThreads : 1;  // of 16 bytes per thread
@@ -72,25 +75,21 @@ __device__ __forceinline__ void walk_tiles(
   // 1.01 and 1.00.)
   auto held = [&](int pid) JF_INLINE { return (uint32_t)pid < (uint32_t)num_pages; };
   auto run_of = [&](int pid) JF_INLINE { return (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv; };
-  const uint32_t k_off = (tid / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
+  const uint32_t k_off = (tid % kOf / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
   auto fetch_k = [&](int slot0, int pid) JF_INLINE {
     const size_t run = run_of(pid);
     const uint8_t* kp = k_codes + (run * P + slot0) * D;
-    if (kOf == kThreads || tid < kOf) {
 #pragma unroll
-      for (int k = 0; k < kPieces; ++k)
-        k_stage[k] = *reinterpret_cast<const u32x4*>(kp + k_off + k * (kThreads / D) * 16 * D);
-    }
+    for (int k = 0; k < kPieces; ++k)
+      k_stage[k] = *reinterpret_cast<const u32x4*>(kp + k_off + k * (kThreads / D) * 16 * D);
     const uint8_t* ep = (lane & 4) ? v_exps : k_exps;
     exps_next = ep[run * (P >> block_shift) + ((slot0 + 16 * (lane & 3)) >> block_shift)];
   };
   auto fetch_v = [&](int slot0, int pid) JF_INLINE {
     const uint8_t* vp = v_codes + (run_of(pid) * P + slot0) * D;
-    if (kOf == kThreads || tid < kOf) {
 #pragma unroll
-      for (int k = 0; k < kPieces; ++k)
-        v_stage[k] = *reinterpret_cast<const u32x4*>(vp + (tid + k * kThreads) * 16);
-    }
+    for (int k = 0; k < kPieces; ++k)
+      v_stage[k] = *reinterpret_cast<const u32x4*>(vp + (tid % kOf + k * kThreads) * 16);
   };
   auto deposit_k = [&](int j) JF_INLINE {
     if (kOf < kThreads && tid >= kOf) return;
@@ -98,7 +97,7 @@ __device__ __forceinline__ void walk_tiles(
     for (int k = 0; k < kPieces; ++k) {
       const int i = tid + k * kThreads;
       // [16 positions][64 dims][half][lane]
-      u32x4* to = tiles_k[j & 1] + i / 64 * 128 + i % 64;
+      u32x4* to = tile_k(j) + i / 64 * 128 + i % 64;
       to[0] = widen8<BF16>(k_stage[k].x, k_stage[k].y), to[64] = widen8<BF16>(k_stage[k].z, k_stage[k].w);
     }
   };
@@ -113,7 +112,7 @@ __device__ __forceinline__ void walk_tiles(
         v_stage[k] &= left ? 0xffffffffu >> (8 * (4 - left)) : 0u;
       }
       // [32 positions][64 dims][dim % 4][lane][16 of the 32]
-      u32x2* to = reinterpret_cast<u32x2*>(tiles_v[j & 1] + (i / D / 2 * C + i % D / 64) * 256 + i % 64) + i / D % 2;
+      u32x2* to = reinterpret_cast<u32x2*>(tile_v(j) + (i / D / 2 * C + i % D / 64) * 256 + i % 64) + i / D % 2;
 #pragma unroll
       for (int dt = 0; dt < 4; ++dt) {
         uint32_t lo, hi;
@@ -140,41 +139,6 @@ __device__ __forceinline__ void walk_tiles(
   uint32_t pf[2][NC][4];  // P as B operands
   int split_e[4];      // where apart: the references of the tile's parts
   bool apart = false;
-
-  // A run of operands that lie one after the other in LDS, each read kAhead
-  // before its products.  (The barriers keep the compiler from reading all of
-  // them at once, which spills.)
-  constexpr int kAhead = 4;
-  auto stream = [&](const u32x4* from, auto first, auto count, auto&& use) JF_INLINE {
-    constexpr int n0 = decltype(first)::value, nn = decltype(count)::value;
-    u32x4 ring[kAhead];
-#pragma unroll
-    for (int p = 0; p < kAhead; ++p) ring[p] = from[(n0 + p) * 64 + lane];
-#pragma unroll
-    for (int p = 0; p < nn; ++p) {
-      const u32x4 a = ring[p % kAhead];
-      if (p + kAhead < nn) ring[p % kAhead] = from[(n0 + p + kAhead) * 64 + lane];
-      use(n0 + p, a);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  auto scores = [&](int j) JF_INLINE {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-#pragma unroll
-      for (int cs = 0; cs < NC; ++cs) s[t][cs] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      // (not 0, so that a hidden score times it stays -inf)
-      f[t] = fmaxf(scale_log2 * power2(__builtin_amdgcn_readlane((int)exps, t) - 127), 1e-37f);
-      ev[t] = __builtin_amdgcn_readlane((int)exps, 4 + t) - 127;
-    }
-    stream(tiles_k[j & 1], std::integral_constant<int, 0>{}, std::integral_constant<int, 8 * C>{},
-           [&](int p, u32x4 a) JF_INLINE {
-             const int t = p / (2 * C), c = p / 2 % C, half = p % 2;
-#pragma unroll
-             for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a, qf[cs][c][half], s[t][cs]);
-           });
-  };
 
   auto softmax = [&](int j, bool on) JF_INLINE {
     const int pos0 = j * kTile;
@@ -264,37 +228,75 @@ __device__ __forceinline__ void walk_tiles(
     }
   };
 
-  auto values = [&](int j) JF_INLINE {
-    auto products = [&](auto t2, const u32x4 (&b)[NC]) {
-      stream(tiles_v[j & 1], std::integral_constant<int, decltype(t2)::value * 4 * C>{},
-             std::integral_constant<int, 4 * C>{}, [&](int p, u32x4 a) JF_INLINE {
-               const int c = p / 4 % C, dt = p % 4;
-#pragma unroll
-               for (int cs = 0; cs < NC; ++cs) acc[cs][c][dt] = mma<false>(a, b[cs], acc[cs][c][dt]);
-             });
+  // The products of turn j: the values of tile j - 1, then the scores of tile j.  Their
+  // operands are one run in LDS, each read kAhead before its products, so that a turn
+  // waits for the first of them only once (as three runs: 2.65 against XX us a tile at
+  // d = 128).  (The barriers keep the compiler from reading all of them at once, which
+  // spills.)
+  constexpr int kAhead = NC == 1 && D <= 128 ? 8 : 4, kV = 8 * C, kAll = 16 * C;
+  auto products = [&](int j) JF_INLINE {
+    const u32x4* const from = lds + (j & 1 ? 2 : 0) * kTileSize + lane;
+    // the scores' operands with the four groups of 16 positions in turn, so that no
+    // product waits for the one before it
+    auto operand = [&](int p) JF_INLINE {
+      const int k = p - kV;
+      return from[64 * (p < kV ? p : kV + k % 4 * (2 * C) + k / 4)];
     };
-    constexpr std::integral_constant<int, 0> t0{};
-    constexpr std::integral_constant<int, 1> t1{};
-    if (!apart) {
+    u32x4 ring[kAhead];
+    if (j > j0 && !apart) {
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        u32x4 b[NC];
+      for (int p = 0; p < kAhead; ++p) ring[p] = operand(p);
 #pragma unroll
-        for (int cs = 0; cs < NC; ++cs) b[cs] = u32x4{pf[t2][cs][0], pf[t2][cs][1], pf[t2][cs][2], pf[t2][cs][3]};
-        if (t2 == 0) products(t0, b); else products(t1, b);
+      for (int p = 0; p < kV; ++p) {
+        const int t2 = p / (4 * C), c = p / 4 % C, dt = p % 4;
+        const u32x4 a = ring[p % kAhead];
+        ring[p % kAhead] = operand(p + kAhead);  // (after the last tile: what is there)
+#pragma unroll
+        for (int cs = 0; cs < NC; ++cs) {
+          const u32x4 b = {pf[t2][cs][0], pf[t2][cs][1], pf[t2][cs][2], pf[t2][cs][3]};
+          acc[cs][c][dt] = mma<false>(a, b, acc[cs][c][dt]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     } else {
+      if (j > j0) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        rescale(reference_step(e_ref, split_e[t]));
-        e_ref = split_e[t];
-        u32x4 b[NC];
+        for (int t = 0; t < 4; ++t) {
+          rescale(reference_step(e_ref, split_e[t]));
+          e_ref = split_e[t];
 #pragma unroll
-        for (int cs = 0; cs < NC; ++cs)
-          b[cs] = t % 2 ? u32x4{0u, 0u, pf[t / 2][cs][2], pf[t / 2][cs][3]}
-                        : u32x4{pf[t / 2][cs][0], pf[t / 2][cs][1], 0u, 0u};
-        if (t < 2) products(t0, b); else products(t1, b);
+          for (int p = 0; p < 4 * C; ++p) {
+            const u32x4 a = operand(t / 2 * 4 * C + p);
+#pragma unroll
+            for (int cs = 0; cs < NC; ++cs) {
+              const u32x4 b = t % 2 ? u32x4{0u, 0u, pf[t / 2][cs][2], pf[t / 2][cs][3]}
+                                    : u32x4{pf[t / 2][cs][0], pf[t / 2][cs][1], 0u, 0u};
+              acc[cs][p / 4][p % 4] = mma<false>(a, b, acc[cs][p / 4][p % 4]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
       }
+#pragma unroll
+      for (int p = 0; p < kAhead; ++p) ring[p] = operand(kV + p);
+    }
+    if (j == j1) return;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int cs = 0; cs < NC; ++cs) s[t][cs] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      // (not 0, so that a hidden score times it stays -inf)
+      f[t] = fmaxf(scale_log2 * power2(__builtin_amdgcn_readlane((int)exps, t) - 127), 1e-37f);
+      ev[t] = __builtin_amdgcn_readlane((int)exps, 4 + t) - 127;
+    }
+#pragma unroll
+    for (int p = kV; p < kAll; ++p) {
+      const int t = (p - kV) % 4, c = (p - kV) / 8, half = (p - kV) / 4 % 2;
+      const u32x4 a = ring[p % kAhead];
+      if (p + kAhead < kAll) ring[p % kAhead] = operand(p + kAhead);
+#pragma unroll
+      for (int cs = 0; cs < NC; ++cs) s[t][cs] = mma<BF16>(a, qf[cs][c][half], s[t][cs]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
@@ -320,50 +322,35 @@ __device__ __forceinline__ void walk_tiles(
     deposit_k(j0);
     fetch_v(slot[1], pid[1]);
     fetch_k(slot[2], pid[2]);
-    // kFar tiles further ahead each line is touched once, so that the fetches find
-    // it in the L2 (2,048 rows over 65,536 positions that the last-level cache does
-    // not hold: 2,815 -> 2,540 us)
-    Place far = at;
-#pragma unroll
-    for (int i = 0; i < kFar; ++i) step(far);
-    int pid_far = page_of(far), slot_far = far.slot;
-    uint32_t touched = 0;
     for (int j = j0; j <= j1; ++j) {
       __syncthreads();  // K of tile j and V of tile j - 1 are in LDS
       const int pid_n = page_of(at);
-      if (tid < D) {
-        asm volatile("" ::"v"(touched));
-        const uint8_t* from = (tid < D / 2 ? k_codes : v_codes) + (run_of(pid_far) * P + slot_far) * D;
-        touched = *reinterpret_cast<const uint32_t*>(from + tid % (D / 2) * 128);
-      }
-      step(far);
-      pid_far = page_of(far), slot_far = far.slot;
-      uint32_t exps_1 = exps_next;
+      uint32_t exps_1;  // of tile j + 1
+      // (Without a condition, past the last tile too, where it carries what nobody reads:
+      // the compiler then knows how many loads are on the way, and waits for the one
+      // that it needs and not for all.  Taken before the next are fetched, exps_1 needs
+      // no copy that would wait at the end of the turn.)
       auto transport = [&]() JF_INLINE {
-        if (j < j1) {
-          deposit_v(j, held(pid[1]) ? 0xffffffffu : 0u);
-          fetch_v(slot[2], pid[2]);
-        }
-        if (j + 1 < j1) {
-          deposit_k(j + 1);
-          fetch_k(slot[3], pid[3]);
-        }
+        deposit_v(j, held(pid[1]) ? 0xffffffffu : 0u);
+        fetch_v(slot[2], pid[2]);
+        deposit_k(j + 1);
+        exps_1 = held(pid[2]) ? exps_next : kZeroExp;
+        asm volatile("" : "+v"(exps_1));
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_k(slot[3], pid[3]);
       };
       if constexpr (late) {
         if (active && j > j0) softmax(j - 1, (uint32_t)pid[0] < (uint32_t)num_pages);
         transport();
       }
       __builtin_amdgcn_s_setprio(1);
-      if (active) {
-        if (j > j0) values(j - 1);
-        if (j < j1) scores(j);
-      }
+      if (active) products(j);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (!late) {
         if (active && j < j1) softmax(j, (uint32_t)pid[1] < (uint32_t)num_pages);
         transport();
       }
-      exps = held(pid[2]) ? exps_1 : kZeroExp;
+      exps = exps_1;
 #pragma unroll
       for (int i = 0; i < 3; ++i) pid[i] = pid[i + 1], slot[i] = slot[i + 1];
       pid[3] = pid_n, slot[3] = at.slot;

@@ -755,10 +755,9 @@ __device__ __forceinline__ void walk_columns(const Args& a, const Cache& in, con
     __device__ __forceinline__ bool hides_some(int pos0) const { return pos0 >= masked; }
     __device__ __forceinline__ bool hides(int cs, int pos) const { return pos >= see[cs]; }
   } sees{masked, see};
-  u32x4(*const lds)[8 * D] = reinterpret_cast<u32x4(*)[8 * D]>(smem);
   walk_tiles<D, BF16, NC>(in.k_codes, in.k_exps, in.v_codes, in.v_exps,
                           tid, table_of(a, in, it), a.Hkv, kv, a.P, a.block_shift, a.num_pages,
-                          it.hi, j0, j1, a.scale_log2, qf, sees, active, lds, lds + 2,
+                          it.hi, j0, j1, a.scale_log2, qf, sees, active, reinterpret_cast<u32x4*>(smem),
                           acc, m, l, e_ref, e_top);
   if (!active) return;
   const float unit = __builtin_ldexpf(1.0f, e_ref);
