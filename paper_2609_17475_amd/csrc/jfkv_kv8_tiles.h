@@ -74,19 +74,21 @@ __device__ __forceinline__ void walk_tiles(
   // 0.99; with a branch around the mask 1.00 and 1.02, around the products instead
   // 1.01 and 1.00.)
   auto held = [&](int pid) JF_INLINE { return (uint32_t)pid < (uint32_t)num_pages; };
-  auto run_of = [&](int pid) JF_INLINE { return (size_t)((uint32_t)pid < (uint32_t)num_pages ? pid : 0) * Hkv + kv; };
+  // (pages times heads are below 2^31)
+  auto run_of = [&](int pid) JF_INLINE { return (uint32_t)(held(pid) ? pid : 0) * (uint32_t)Hkv + (uint32_t)kv; };
+  auto place = [&](int slot0, int pid) JF_INLINE { return ((uint64_t)run_of(pid) * (uint32_t)P + (uint32_t)slot0) * D; };
   const uint32_t k_off = (tid % kOf / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
   auto fetch_k = [&](int slot0, int pid) JF_INLINE {
-    const size_t run = run_of(pid);
-    const uint8_t* kp = k_codes + (run * P + slot0) * D;
+    const uint8_t* kp = k_codes + place(slot0, pid);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
       k_stage[k] = *reinterpret_cast<const u32x4*>(kp + k_off + k * (kThreads / D) * 16 * D);
     const uint8_t* ep = (lane & 4) ? v_exps : k_exps;
-    exps_next = ep[run * (P >> block_shift) + ((slot0 + 16 * (lane & 3)) >> block_shift)];
+    exps_next = ep[(uint64_t)run_of(pid) * (uint32_t)(P >> block_shift) +
+                   (uint32_t)((slot0 + 16 * (lane & 3)) >> block_shift)];
   };
   auto fetch_v = [&](int slot0, int pid) JF_INLINE {
-    const uint8_t* vp = v_codes + (run_of(pid) * P + slot0) * D;
+    const uint8_t* vp = v_codes + place(slot0, pid);
 #pragma unroll
     for (int k = 0; k < kPieces; ++k)
       v_stage[k] = *reinterpret_cast<const u32x4*>(vp + (tid % kOf + k * kThreads) * 16);
@@ -341,15 +343,14 @@ __device__ __forceinline__ void walk_tiles(
       };
       if constexpr (late) {
         if (active && j > j0) softmax(j - 1, (uint32_t)pid[0] < (uint32_t)num_pages);
-        transport();
       }
       __builtin_amdgcn_s_setprio(1);
       if (active) products(j);
       __builtin_amdgcn_s_setprio(0);
       if constexpr (!late) {
         if (active && j < j1) softmax(j, (uint32_t)pid[1] < (uint32_t)num_pages);
-        transport();
       }
+      transport();
       exps = exps_1;
 #pragma unroll
       for (int i = 0; i < 3; ++i) pid[i] = pid[i + 1], slot[i] = slot[i + 1];
