@@ -35,13 +35,15 @@ using tiles::kTile;
 using tiles::walk_tiles;
 
 constexpr int kRow = 32;        // positions that a wave of the row walk takes at a time (in one page)
-constexpr int kRowWaves = 4;
-constexpr int kRowBlocks = 2;   // blocks of the row walk per CU
-constexpr int kRowThreads = 64 * kRowWaves, kTileThreads = tiles::kThreads;
+constexpr int kRowWaves = 4, kTileWaves = tiles::kWaves;
+constexpr int kRowThreads = 64 * kRowWaves, kTileThreads = 64 * kTileWaves;
 constexpr int kMinRows = 2;     // rows per wave below which a unit is not cut
 constexpr int kRowCols = 64;    // columns of a group that are walked by rows at most
 constexpr int kSub = 32;        // columns that can have a chunk of their own
 constexpr float kLn2 = 0.69314718055994530942f;
+
+// What a kernel takes: the groups' shared positions, the requests' own, or both.
+enum Part { kGroups, kOwn, kBoth };
 
 // How a chunk of columns is computed: by rows, one or two sets of 16 columns for all of
 // a block's waves, or by tiles, one or two sets for each of eight waves.
@@ -61,6 +63,13 @@ __host__ __device__ constexpr int cost_of(int kind) {
 }
 __host__ __device__ constexpr int start_of(int kind) { return kind >= kTiles1 ? 60 : 30; }
 
+// Blocks of the row walk per CU.  One set of columns leaves room for more, which hides
+// more of the loads (64 requests of 4,096 positions of their own, 32/8 heads of 128:
+// 133 us with two, XX with three).
+__host__ __device__ constexpr int row_blocks(int D, bool one_set) {
+  return one_set ? (D > 128 ? 2 : D > 64 ? 3 : 4) : 2;
+}
+
 // Values that are the same in all lanes, to scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -79,7 +88,8 @@ struct Args {
   int2* info;     // (first record, records) of each unit: groups', then requests'
   int B, G, sq, Hq, Hkv, gq, P, block_shift, num_pages, max_pages;
   int group_units, own_kind, chunks, own_cols;  // kind, chunks and columns of a request's own units
-  int64_t row_recs, own_recs;  // where groups' records by rows and requests' records begin (floats)
+  int group_cols;    // columns of a group's record slot
+  int64_t own_recs;  // where requests' records begin (floats; groups' are before)
   float scale_log2;
   uint32_t flip;  // a negative scale negates the queries instead
 };
@@ -138,12 +148,16 @@ struct Item {
   // cost of a unit but for its start
   __device__ __forceinline__ int64_t work() const { return (int64_t)steps() * cost_of(kind); }
 };
-// (An item of the other kernel is empty.)
-template <int D, bool TILES>
+// Items of a kernel, and item i of them.
+template <int PART>
+__device__ __forceinline__ int items_of(const Args& a) {
+  return (PART == kOwn ? 0 : 2 * a.G) + (PART == kGroups ? 0 : a.B);
+}
+template <int D, int PART>
 __device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i) {
   Item t;
   const int pairs = a.gq * a.sq;
-  if (i < 2 * a.G) {
+  if (PART == kGroups || (PART == kBoth && i < 2 * a.G)) {
     constexpr int W = widest(D);
     const int g = i >> 1;
     t.request = batch.first(g);
@@ -151,10 +165,9 @@ __device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i
     t.col0 = i & 1 ? full : 0;
     t.cols = i & 1 ? cols : full;
     t.kind = i & 1 ? kind_of(D, cols - full) : kind_of(D, W);
-    t.lo = 0;
-    t.hi = t.cols > t.col0 && (t.kind >= kTiles1) == TILES ? batch.shared(g) : 0;
+    t.lo = 0, t.hi = t.cols > t.col0 ? batch.shared(g) : 0;
   } else {
-    t.request = i - 2 * a.G;
+    t.request = PART == kOwn ? i : i - 2 * a.G;
     t.col0 = 0, t.cols = pairs;
     t.lo = batch.valid ? batch.shared(batch.of(t.request)) : 0, t.hi = batch.length(t.request);
     t.kind = a.own_kind;
@@ -223,7 +236,7 @@ struct Plan {
   }
 
   // All threads: the block's first segment; false: there is none.
-  template <int D, bool TILES>
+  template <int D, int PART>
   __device__ __forceinline__ bool begin(const Args& g, const int32_t* g_lens) {
     const int tid = threadIdx.x, lane = tid & 63, team = uniform(tid >> 6), blocks = gridDim.x;
     Batch b = batch(g, g_lens, true);
@@ -242,12 +255,12 @@ struct Plan {
     b.valid = !__syncthreads_or(bad);
 
     // all items' work, units and starts
-    const int n = TILES ? 2 * g.G : 2 * g.G + g.B;
+    const int n = items_of<PART>(g);
     int64_t work = 0;
     int count = 0, begins = 0, units_here = 0, work_here = 0;
     Item t = {};
     for (int i = tid; i < n; i += T) {
-      t = item_of<D, TILES>(g, b, i);
+      t = item_of<D, PART>(g, b, i);
       const int64_t w = t.work();
       const int m = w ? t.chunks() * g.Hkv : 0;
       work += w * m, count += m, begins += m * start_of(t.kind);
@@ -264,7 +277,7 @@ struct Plan {
     for (int w = 0; w < kTeams; ++w) work += sum[w], count += units[w], begins += starts[w];
     work = uniform(work), count = uniform(count), begins = uniform(begins);
     if (count == 0) return false;
-    constexpr int kLeast = TILES ? 2 * cost_of(kTiles1) : cost_of(kRows1) * kRowWaves * kMinRows;
+    constexpr int kLeast = cost_of(kRows1) * kTeams * kMinRows;
     if (2 * count > blocks || n > T || work >= 0x40000000) {  // the line
       if (tid == 0) {
         a = g;
@@ -274,7 +287,7 @@ struct Plan {
         upto[T] = 0;  // (no window yet)
       }
       __syncthreads();
-      return next<D, TILES>(g_lens);
+      return next<D, PART>(g_lens);
     }
 
     // Shares: as many as there are blocks, or less.  Their length lies between work /
@@ -315,7 +328,7 @@ struct Plan {
       const int u = (int)(((float)j + 0.5f) / (float)each), share = j - u * each;  // (both below 2^16)
       const uint32_t steps = t.steps(), size = (steps + each - 1) / (uint32_t)each;
       const int r0 = (int)min(share * size, steps), r1 = (int)min(r0 + size, steps);
-      put<D, TILES>(g, t, tid, u, r0, r1, (int)((steps + size - 1) / size));
+      put<D, PART>(g, t, tid, u, r0, r1, (int)((steps + size - 1) / size));
     }
     __syncthreads();
     return uniform(segment.r0) < uniform(segment.r1);
@@ -323,34 +336,33 @@ struct Plan {
 
   // Steps r0 .. r1 - 1 of unit u of item i, which leaves `records` records, the first of
   // them by the block that has its first step.
-  template <int D, bool TILES>
+  template <int D, int PART>
   __device__ __forceinline__ void put(const Args& g, const Item& it, int i, int u, int r0, int r1,
                                       int records) {
     const int chunk = (int)(((float)u + 0.5f) / (float)g.Hkv), kv = u - chunk * g.Hkv;  // (u below 2^17)
     const int col = it.col0 + (chunk << width_log2(it.kind));
     int id, first_col, entry;
     int64_t rec;
-    if (TILES || i < 2 * g.G) {
+    const int64_t block = blockIdx.x;
+    if (PART == kGroups || (PART == kBoth && i < 2 * g.G)) {
       group_place<D>(g, it.request, i >> 1, col, kv, id, first_col, entry);
-      const int64_t slot = (int64_t)id + blockIdx.x;
-      rec = TILES ? (slot * widest(D) + first_col) * (D + 4)
-                  : g.row_recs + (slot * kRowCols + first_col % kRowCols) * (D + 4);
+      rec = ((id + block) * g.group_cols + (first_col & (g.group_cols - 1))) * (D + 4);
     } else {
       own_place<D>(g, it.request, chunk, kv, id, entry);
-      rec = g.own_recs + ((int64_t)id + blockIdx.x) * (g.own_cols * (D + 4));
+      rec = g.own_recs + (id + block) * (g.own_cols * (D + 4));
     }
     if (r0 == 0 && r1 > 0) g.info[entry] = make_int2(id + blockIdx.x, records);
     segment = Segment{it, col, kv, r0, r1, rec};
   }
 
   // All threads: the block's next segment; false: none is left.
-  template <int D, bool TILES>
+  template <int D, int PART>
   __device__ __forceinline__ bool next(const int32_t* g_lens) {
     if (uniform((int)state.apart)) return false;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
     const int lane = tid & 63, team = uniform(tid >> 6);
-    const int n = uniform(TILES ? 2 * a.G : 2 * a.G + a.B);
+    const int n = uniform(items_of<PART>(a));
     for (;;) {
       const int64_t x = uniform(state.x);
       int window = uniform(state.window);
@@ -360,7 +372,7 @@ struct Plan {
         window += T;
         if (window >= n) return false;
         const bool mine = window + tid < n;
-        if (n > T && mine) items[tid] = item_of<D, TILES>(a, batch(a, g_lens, state.valid), window + tid);
+        if (n > T && mine) items[tid] = item_of<D, PART>(a, batch(a, g_lens, state.valid), window + tid);
         int64_t to = mine ? span(items[tid]) * (items[tid].chunks() * a.Hkv) : 0;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -388,7 +400,7 @@ struct Plan {
         const int r1 = end >= at + work ? steps : (int)whole(max(end - at, (int64_t)0) + cost - 1, cost);
         // (the last step's piece, counted from this block's)
         const int more = end >= at + work ? 0 : (int)whole(at + work - cost - (end - piece), piece);
-        put<D, TILES>(a, it, window + tid, u, r0, r1, 1 + more);
+        put<D, PART>(a, it, window + tid, u, r0, r1, 1 + more);
         state.x = start + length;
       }
       __syncthreads();
@@ -437,7 +449,7 @@ __device__ __forceinline__ Table table_of(const Args& a, const Cache& in, const 
 
 // Steps r0 .. r1 - 1 (counted from the item's first) of the chunk of columns from c0 on,
 // its record to rec, by rows.
-template <int D, bool BF16, int CS>
+template <int D, bool BF16, int CS, int WAVES>
 __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const Batch& batch,
                                           const Item& it, int c0, int kv,
                                           int r0, int r1, float* rec, float* smem) {
@@ -445,12 +457,12 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
   constexpr int kPart = D + 4;  // floats of a partial: o, m, l (16-byte rows)
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));  // (opaque: what depends on it is not held from one segment to the next)
-  __builtin_assume(tid >= 0 && tid < kRowThreads);
+  __builtin_assume(tid >= 0 && tid < 64 * WAVES);
   const int lane = tid & 63, n = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int P = a.P, ncols = min(16 * CS, it.cols - c0);
 
-  // ---- page walk: the wave takes rows r0 + wave, + kRowWaves, ...  A row's registers
+  // ---- page walk: the wave takes rows r0 + wave, + WAVES, ...  A row's registers
   // are refilled with the next row, K's as soon as the scores are formed and V's after
   // the value products.  Page IDs are read one turn before the loads.
   const Table table = table_of(a, in, it);
@@ -484,7 +496,7 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
 
   Row<D> w;
   int r = base + r0 + wave;
-  int pid = page_of(r), ahead = page_of(r + kRowWaves);
+  int pid = page_of(r), ahead = page_of(r + WAVES);
   fetch_k(w, r, pid);
   fetch_v(w, r, pid);
 
@@ -504,7 +516,7 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        if (!kQLds || wave == (cs * C + c) % kRowWaves) {
+        if (!kQLds || wave == (cs * C + c) % WAVES) {
           const u32x4 x = *reinterpret_cast<const u32x4*>(qp + 64 * c + 16 * g + 8 * j) ^ a.flip;
           if (kQLds)
             s_q[64 * ((cs * C + c) * 2 + j) + lane] = x;
@@ -662,16 +674,16 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
     }
   };
 
-  for (; r <= last; r += kRowWaves) {
+  for (; r <= last; r += WAVES) {
     const bool on = (uint32_t)pid < (uint32_t)a.num_pages;
     float s[CS][2][4];
     int ev[2];
     scores(w, r, s, ev);
-    fetch_k(w, r + kRowWaves, ahead);
+    fetch_k(w, r + WAVES, ahead);
     if (on) attend(w, r, s, ev);
-    fetch_v(w, r + kRowWaves, ahead);
+    fetch_v(w, r + WAVES, ahead);
     pid = ahead;
-    ahead = page_of(r + 2 * kRowWaves);
+    ahead = page_of(r + 2 * WAVES);
   }
 
   // ---- merge the waves in LDS, one set of columns after the other: o (units 1), m, l
@@ -693,18 +705,18 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
       if (g == 0) mine[D] = m[cs], mine[D + 1] = den;
     }
     __syncthreads();
-    for (int i = tid; i < here * (D / 4); i += kRowThreads) {
+    for (int i = tid; i < here * (D / 4); i += 64 * WAVES) {
       const int at = i / (D / 4), d4 = i % (D / 4);
       const float* const part = smem + at * kPart;
-      float mw[kRowWaves], M = -INFINITY, sum = 0.0f;
+      float mw[WAVES], M = -INFINITY, sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < kRowWaves; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         mw[w] = part[w * wide + D];
         M = fmaxf(M, mw[w]);
       }
       f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int w = 0; w < kRowWaves; ++w) {
+      for (int w = 0; w < WAVES; ++w) {
         const float f = mw[w] == -INFINITY ? 0.0f : exp2_(mw[w] - M);
         num += *reinterpret_cast<const f32x4*>(part + w * wide + 4 * d4) * f;
         sum = fmaf(f, part[w * wide + D + 1], sum);
@@ -777,8 +789,9 @@ __device__ __forceinline__ void walk_columns(const Args& a, const Cache& in, con
   }
 }
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(kRowThreads, kRowBlocks) void kv8_shared_rows_kernel(
+// Requests' own positions (SETS of 16 columns), and groups' in small batches.
+template <int D, bool BF16, int PART, int SETS>
+__global__ __launch_bounds__(kRowThreads, row_blocks(D, PART == kOwn && SETS == 1)) void kv8_shared_rows_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
     const uint16_t* __restrict__ q, const int32_t* __restrict__ tables,
@@ -786,19 +799,20 @@ __global__ __launch_bounds__(kRowThreads, kRowBlocks) void kv8_shared_rows_kerne
   extern __shared__ __align__(1024) float smem[];
   __shared__ Plan<kRowThreads> plan;
   const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables};
-  for (bool more = plan.begin<D, false>(a, lens); more; more = plan.next<D, false>(lens)) {
+  for (bool more = plan.begin<D, PART>(a, lens); more; more = plan.next<D, PART>(lens)) {
     const Args f = plan.args();
     const Segment t = plan.part();
     const Batch batch = plan.batch(f, lens, plan.state.valid);
-    if (t.it.kind == kRows1)
-      walk_rows<D, BF16, 1>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+    if (PART == kOwn ? SETS == 1 : t.it.kind == kRows1)
+      walk_rows<D, BF16, 1, kRowWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
     else
-      walk_rows<D, BF16, 2>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+      walk_rows<D, BF16, 2, kRowWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
   }
 }
 
+// Groups' shared positions.
 template <int D, bool BF16>
-__global__ __launch_bounds__(kTileThreads) void kv8_shared_tiles_kernel(
+__global__ __launch_bounds__(kTileThreads) void kv8_shared_groups_kernel(
     const uint8_t* __restrict__ k_codes, const uint8_t* __restrict__ k_exps,
     const uint8_t* __restrict__ v_codes, const uint8_t* __restrict__ v_exps,
     const uint16_t* __restrict__ q, const int32_t* __restrict__ tables,
@@ -806,15 +820,20 @@ __global__ __launch_bounds__(kTileThreads) void kv8_shared_tiles_kernel(
   extern __shared__ __align__(1024) float smem[];
   __shared__ Plan<kTileThreads> plan;
   const Cache in{k_codes, k_exps, v_codes, v_exps, q, tables};
-  for (bool more = plan.begin<D, true>(a, lens); more; more = plan.next<D, true>(lens)) {
+  for (bool more = plan.begin<D, kGroups>(a, lens); more; more = plan.next<D, kGroups>(lens)) {
     const Args f = plan.args();
     const Segment t = plan.part();
     const Batch batch = plan.batch(f, lens, plan.state.valid);
     constexpr int kMost = widest(D) / 128;
-    if (kMost == 1 || t.it.kind == kTiles1)
-      walk_columns<D, BF16, 1>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+    float* const rec = recs + t.rec;
+    if (t.it.kind == kRows1)
+      walk_rows<D, BF16, 1, kTileWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
+    else if (t.it.kind == kRows2)
+      walk_rows<D, BF16, 2, kTileWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
+    else if (kMost == 1 || t.it.kind == kTiles1)
+      walk_columns<D, BF16, 1>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
     else
-      walk_columns<D, BF16, kMost>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+      walk_columns<D, BF16, kMost>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
   }
 }
 
@@ -824,7 +843,7 @@ constexpr int kJoinWaves = 4;
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
     const float* __restrict__ recs, const int32_t* __restrict__ lens, uint16_t* __restrict__ out,
-    float* __restrict__ lse, const Args a, int tile_blocks, int row_blocks) {
+    float* __restrict__ lse, const Args a, int group_blocks, int own_blocks) {
   constexpr int kPart = D + 4, kAt = 4;
   __shared__ f32x4 s_num[kJoinWaves][64];
   __shared__ f32x2 s_ml[kJoinWaves][64];
@@ -878,17 +897,16 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
     const int off = (col - (in_full ? 0 : full)) & (width_of(kind) - 1);  // in its chunk
     group_place<D>(a, from, group, col - off, kv, id, at, entry);
     const int2 in = a.info[entry];
-    const bool by_tiles = kind >= kTiles1;
-    const int64_t stride = (int64_t)(by_tiles ? W : kRowCols) * kPart;
-    add(recs + (by_tiles ? 0 : a.row_recs) + in.x * stride + (int64_t)((by_tiles ? at : at % kRowCols) + off) * kPart,
-        stride, min(in.y, by_tiles ? tile_blocks : row_blocks));
+    const int64_t stride = (int64_t)a.group_cols * kPart;
+    add(recs + in.x * stride + (int64_t)((at & (a.group_cols - 1)) + off) * kPart, stride,
+        min(in.y, group_blocks));
   }
   if (len > shared) {
     const int width = width_of(a.own_kind);
     own_place<D>(a, b, pair / width, kv, id, entry);
     const int2 in = a.info[entry];
     const int64_t stride = (int64_t)a.own_cols * kPart;
-    add(recs + a.own_recs + in.x * stride + (int64_t)(pair % width) * kPart, stride, min(in.y, row_blocks));
+    add(recs + a.own_recs + in.x * stride + (int64_t)(pair % width) * kPart, stride, min(in.y, own_blocks));
   }
   s_num[wave][lane] = num;
   s_ml[wave][lane] = f32x2{M, den};
@@ -914,25 +932,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
 
 // How the workspace is laid out.
 struct Layout {
-  int tile_blocks, row_blocks, group_units, own_kind, chunks, own_cols;
-  int64_t row_recs, own_recs;
+  bool both;  // one kernel for groups and requests
+  int group_blocks, own_blocks, group_units, group_cols, own_kind, chunks, own_cols;
+  int64_t own_recs;
   size_t recs, bytes;
 };
 Layout layout_of(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq) {
   const int D = L.head_dim, Hkv = L.num_kv_heads, pairs = Hq / Hkv * sq, W = widest(D);
   Layout p;
-  p.tile_blocks = (int64_t)B * pairs > kRowCols ? num_cus() : 0;  // (else no group has so many columns)
-  p.row_blocks = kRowBlocks * num_cus();
-  p.group_units = (int)(((int64_t)B * pairs / W + G + 1) * Hkv);
+  p.both = (int64_t)B * pairs <= kRowCols;  // (no group has more columns)
   p.own_kind = pairs <= 16 ? kRows1 : kRows2;
+  p.own_blocks = row_blocks(D, !p.both && p.own_kind == kRows1) * num_cus();
+  p.group_blocks = p.both ? p.own_blocks : num_cus();
+  p.group_cols = p.both ? kRowCols : W;
+  p.group_units = (int)(((int64_t)B * pairs / W + G + 1) * Hkv);
   const int width = width_of(p.own_kind);
   p.own_cols = std::min(pairs, width);
   p.chunks = (pairs + width - 1) / width;
   const int64_t own_units = (int64_t)B * p.chunks * Hkv;
-  p.row_recs = p.tile_blocks ? ((int64_t)p.group_units + p.tile_blocks) * W * (D + 4) : 0;
-  p.own_recs = p.row_recs + ((int64_t)p.group_units + p.row_blocks) * kRowCols * (D + 4);
+  p.own_recs = ((int64_t)p.group_units + p.group_blocks) * p.group_cols * (D + 4);
   p.recs = ((size_t)((int64_t)p.group_units * (W / kSub) + own_units) * sizeof(int2) + 15) / 16 * 16;
-  p.bytes = p.recs + (size_t)(p.own_recs + (own_units + p.row_blocks) * p.own_cols * (D + 4)) * sizeof(float);
+  p.bytes = p.recs + (size_t)(p.own_recs + (own_units + p.own_blocks) * p.own_cols * (D + 4)) * sizeof(float);
   return p;
 }
 
@@ -949,19 +969,23 @@ hipError_t launch_t(const Cache& in, const int32_t* lens, const Args& a, const L
                        in.v_codes, in.v_exps, in.q, in.tables, lens, recs, a);
     return hipGetLastError();
   };
-  if (p.tile_blocks) {
-    const hipError_t e = go(kv8_shared_tiles_kernel<D, BF16>, p.tile_blocks, kTileThreads,
-                            4 * 8 * D * sizeof(u32x4));
-    if (e != hipSuccess) return e;
-  }
   // (the waves' merge; the queries before it take less)
-  const hipError_t e = go(kv8_shared_rows_kernel<D, BF16>, p.row_blocks, kRowThreads,
-                          sizeof(float) * kRowWaves * 16 * (D + 4));
+  const size_t merge = sizeof(float) * kRowWaves * 16 * (D + 4);
+  hipError_t e = hipSuccess;
+  if (p.both) {
+    e = go(kv8_shared_rows_kernel<D, BF16, kBoth, 2>, p.own_blocks, kRowThreads, merge);
+  } else {
+    e = go(kv8_shared_groups_kernel<D, BF16>, p.group_blocks, kTileThreads,
+           std::max(4 * 8 * D * sizeof(u32x4), 2 * merge));
+    if (e == hipSuccess)
+      e = p.own_kind == kRows1 ? go(kv8_shared_rows_kernel<D, BF16, kOwn, 1>, p.own_blocks, kRowThreads, merge)
+                               : go(kv8_shared_rows_kernel<D, BF16, kOwn, 2>, p.own_blocks, kRowThreads, merge);
+  }
   if (e != hipSuccess) return e;
   const int runs = a.gq * a.sq * (D / 4);
   hipLaunchKernelGGL((kv8_shared_join_kernel<D, BF16>), dim3((runs + 63) / 64, a.Hkv, a.B),
                      dim3(64 * kJoinWaves), 0, stream, recs, lens, static_cast<uint16_t*>(out), lse,
-                     a, p.tile_blocks, p.row_blocks);
+                     a, p.group_blocks, p.own_blocks);
   return hipGetLastError();
 }
 
@@ -987,7 +1011,7 @@ hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
   a.first = group_start, a.shared = shared_lens, a.info = static_cast<int2*>(ws);
   a.B = B, a.G = G, a.sq = sq, a.Hq = Hq, a.Hkv = L.num_kv_heads, a.gq = Hq / L.num_kv_heads, a.P = L.page_size;
   a.block_shift = shift, a.num_pages = L.num_pages, a.max_pages = max_pages;
-  a.group_units = p.group_units, a.own_kind = p.own_kind, a.chunks = p.chunks, a.own_cols = p.own_cols, a.row_recs = p.row_recs, a.own_recs = p.own_recs;
+  a.group_units = p.group_units, a.own_kind = p.own_kind, a.chunks = p.chunks, a.own_cols = p.own_cols, a.group_cols = p.group_cols, a.own_recs = p.own_recs;
   a.scale_log2 = std::fabs(softmax_scale) * tiles::kLog2e;
   a.flip = softmax_scale < 0.0f ? 0x80008000u : 0u;
   float* const recs = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.recs);
