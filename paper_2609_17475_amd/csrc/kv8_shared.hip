@@ -194,7 +194,7 @@ __device__ __forceinline__ void own_place(const Args& a, int request, int chunk,
 // Where a block is on the line: at x, up to end; the window of items that is summed up
 // begins with item `window`.
 struct State {
-  int64_t x, end, piece;
+  int64_t x, begin, end, piece;
   int window;
   bool valid, apart;
 };
@@ -277,13 +277,13 @@ struct Plan {
     for (int w = 0; w < kTeams; ++w) work += sum[w], count += units[w], begins += starts[w];
     work = uniform(work), count = uniform(count), begins = uniform(begins);
     if (count == 0) return false;
-    constexpr int kLeast = cost_of(kRows1) * kTeams * kMinRows;
+    constexpr int kLeast = cost_of(kRows1) * kRowWaves * kMinRows;
     if (2 * count > blocks || n > T || work >= 0x40000000) {  // the line
       if (tid == 0) {
         a = g;
         const int64_t piece = max(whole(work + begins, blocks) + 1, (int64_t)kLeast);
         const int64_t from = blockIdx.x * piece;
-        state = State{from, min(from + piece, work + begins), piece, -T, b.valid, false};
+        state = State{from, from, min(from + piece, work + begins), piece, -T, b.valid, false};
         upto[T] = 0;  // (no window yet)
       }
       __syncthreads();
@@ -397,9 +397,12 @@ struct Plan {
         const int u = in < length ? 0 : (int)whole(in, length);
         const int64_t start = x - in + u * length, at = start + start_of(it.kind), work = it.work();
         const int r0 = (int)whole(max(x - at, (int64_t)0) + cost - 1, cost);
-        const int r1 = end >= at + work ? steps : (int)whole(max(end - at, (int64_t)0) + cost - 1, cost);
-        // (the last step's piece, counted from this block's)
-        const int more = end >= at + work ? 0 : (int)whole(at + work - cost - (end - piece), piece);
+        int r1 = steps, more = 0;
+        if (end < at + work) {
+          r1 = (int)whole(max(end - at, (int64_t)0) + cost - 1, cost);
+          // the last step's piece, counted from this block's
+          more = (int)whole(at + work - cost - state.begin, piece);
+        }
         put<D, PART>(a, it, window + tid, u, r0, r1, 1 + more);
         state.x = start + length;
       }
@@ -449,7 +452,7 @@ __device__ __forceinline__ Table table_of(const Args& a, const Cache& in, const 
 
 // Steps r0 .. r1 - 1 (counted from the item's first) of the chunk of columns from c0 on,
 // its record to rec, by rows.
-template <int D, bool BF16, int CS, int WAVES>
+template <int D, bool BF16, int CS, int WAVES, bool ONCE>
 __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const Batch& batch,
                                           const Item& it, int c0, int kv,
                                           int r0, int r1, float* rec, float* smem) {
@@ -472,6 +475,10 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
   auto run_of = [&](int pid) {
     return (size_t)((uint32_t)pid < (uint32_t)a.num_pages ? pid : 0) * a.Hkv + kv;
   };
+  auto load = [](const uint8_t* from) {  // (ONCE: no other block reads it)
+    const u32x4* const p = reinterpret_cast<const u32x4*>(from);
+    return ONCE ? __builtin_nontemporal_load(p) : *p;
+  };
   auto fetch_k = [&](Row<D>& w, int r, int pid) {
     const int slot0 = min(r, last) * kRow % P;
     const size_t run = run_of(pid);
@@ -480,7 +487,7 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        w.k[t][c] = *reinterpret_cast<const u32x4*>(kp + koff + t * 16 * D + c * 64);
+        w.k[t][c] = load(kp + koff + t * 16 * D + c * 64);
     const uint8_t* ep = (lane & 2) ? in.v_exps : in.k_exps;
     w.exps = ep[run * (P >> a.block_shift) + ((slot0 + 16 * (lane & 1)) >> a.block_shift)];
   };
@@ -491,7 +498,7 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        w.v[t][c] = *reinterpret_cast<const u32x4*>(vp + voff + t * 16 * D + c * 1024);
+        w.v[t][c] = load(vp + voff + t * 16 * D + c * 1024);
   };
 
   Row<D> w;
@@ -804,9 +811,9 @@ __global__ __launch_bounds__(kRowThreads, row_blocks(D, PART == kOwn && SETS == 
     const Segment t = plan.part();
     const Batch batch = plan.batch(f, lens, plan.state.valid);
     if (PART == kOwn ? SETS == 1 : t.it.kind == kRows1)
-      walk_rows<D, BF16, 1, kRowWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+      walk_rows<D, BF16, 1, kRowWaves, PART == kOwn>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
     else
-      walk_rows<D, BF16, 2, kRowWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
+      walk_rows<D, BF16, 2, kRowWaves, PART == kOwn>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, recs + t.rec, smem);
   }
 }
 
@@ -827,9 +834,9 @@ __global__ __launch_bounds__(kTileThreads) void kv8_shared_groups_kernel(
     constexpr int kMost = widest(D) / 128;
     float* const rec = recs + t.rec;
     if (t.it.kind == kRows1)
-      walk_rows<D, BF16, 1, kTileWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
+      walk_rows<D, BF16, 1, kTileWaves, false>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
     else if (t.it.kind == kRows2)
-      walk_rows<D, BF16, 2, kTileWaves>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
+      walk_rows<D, BF16, 2, kTileWaves, false>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
     else if (kMost == 1 || t.it.kind == kTiles1)
       walk_columns<D, BF16, 1>(f, in, batch, t.it, t.col, t.kv, t.r0, t.r1, rec, smem);
     else
@@ -851,6 +858,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   const int kv = blockIdx.y, b = blockIdx.z, gq = a.gq, pairs = gq * a.sq;
 
   Batch batch{a.first, a.shared, lens, nullptr, nullptr, nullptr, a.G, a.max_pages * a.P, false, true};
+  const int i = blockIdx.x * 64 + lane, pair = min(i / (D / 4), pairs - 1), d4 = i % (D / 4);
+  // what does not wait for the groups: the request's own records
+  int id, at, entry;
+  own_place<D>(a, b, pair >> width_log2(a.own_kind), kv, id, entry);
+  const int2 own = a.info[entry];  // (nothing of use where it has none)
+  const int len = batch.length(b);
   int bad = 0;
   for (int i = tid; i <= a.G; i += 64 * kJoinWaves) {
     const int at = a.first[i];
@@ -859,9 +872,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   }
   batch.valid = !__syncthreads_or(bad);
   const int group = batch.valid ? batch.of(b) : 0;
-  const int shared = batch.valid ? batch.shared(group) : 0, len = batch.length(b);
+  const int shared = batch.valid ? batch.shared(group) : 0;
 
-  const int i = blockIdx.x * 64 + lane, pair = min(i / (D / 4), pairs - 1), d4 = i % (D / 4);
   f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
   float M = -INFINITY, den = 0.0f;
   auto add = [&](const float* from, int64_t stride, int count) {
@@ -888,7 +900,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
       M = mx;
     }
   };
-  int id, at, entry;
   if (shared > 0) {
     constexpr int W = widest(D);
     const int from = batch.first(group), cols = (batch.first(group + 1) - from) * pairs;
@@ -902,11 +913,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
         min(in.y, group_blocks));
   }
   if (len > shared) {
-    const int width = width_of(a.own_kind);
-    own_place<D>(a, b, pair / width, kv, id, entry);
-    const int2 in = a.info[entry];
     const int64_t stride = (int64_t)a.own_cols * kPart;
-    add(recs + a.own_recs + in.x * stride + (int64_t)(pair % width) * kPart, stride, min(in.y, own_blocks));
+    add(recs + a.own_recs + own.x * stride + (int64_t)(pair & (width_of(a.own_kind) - 1)) * kPart, stride,
+        min(own.y, own_blocks));
   }
   s_num[wave][lane] = num;
   s_ml[wave][lane] = f32x2{M, den};
