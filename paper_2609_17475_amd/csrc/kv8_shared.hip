@@ -64,8 +64,10 @@ __host__ __device__ constexpr int cost_of(int kind) {
 __host__ __device__ constexpr int start_of(int kind) { return kind >= kTiles1 ? 60 : 30; }
 
 // Blocks of the row walk per CU.  One set of columns leaves room for more, which hides
-// more of the loads (64 requests of 4,096 positions of their own, 32/8 heads of 128:
-// 133 us with two, XX with three).
+// more of a unit's start (three in place of two, 32/8 heads of 128: 256 requests of 300
+// positions of their own 79 -> 72 us, 64 of 300 40 -> 37; 64 of 4,096 133 -> 137).  A
+// kernel that takes groups as well has two: its second walk would spill (16 requests over
+// 8,192 shared positions 24.2 -> 26.9 us with three).
 __host__ __device__ constexpr int row_blocks(int D, bool one_set) {
   return one_set ? (D > 128 ? 2 : D > 64 ? 3 : 4) : 2;
 }
@@ -219,6 +221,7 @@ struct Plan {
   Item items[T];
   int64_t sum[kTeams];
   int units[kTeams], starts[kTeams];
+  float lengths[kTeams];
   int32_t first[T + 1], shared[T], lens[2 * T];
 
   __device__ __forceinline__ Batch batch(const Args& g, const int32_t* g_lens, bool valid) const {
@@ -294,24 +297,24 @@ struct Plan {
     // blocks and work / (blocks - count); each wave counts those of one length, the
     // least that are not too many are taken.
     const float low = (float)work / (float)blocks, high = (float)work / (float)(blocks - count) * 1.0001f + 1.0f;
-    auto length = [&](int w) { return fmaxf(low + (high - low) * ((float)w / (kTeams - 1)), (float)kLeast); };
+    const float length = fmaxf(low + (high - low) * ((float)team / (kTeams - 1)), (float)kLeast);
     __syncthreads();  // (`units` is written again)
     int many = 0;
     for (int i = lane; i < n; i += 64) {
       const Item u = items[i];
       const int w = (int)u.work();
-      if (w) many += shares(w, length(team)) * (u.chunks() * g.Hkv);
+      if (w) many += shares(w, length) * (u.chunks() * g.Hkv);
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) many += __shfl_xor(many, o);
-    if (lane == 0) units[team] = many;
+    if (lane == 0) units[team] = many, lengths[team] = length;
     __syncthreads();
     int pick = kTeams - 1;
 #pragma unroll
     for (int w = kTeams - 2; w >= 0; --w)
       if (units[w] <= blocks) pick = w;
     // the block's share: one thread's item has it
-    const int each = shares(work_here, length(pick)), all = each * units_here;
+    const int each = shares(work_here, lengths[pick]), all = each * units_here;
     int to = all;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -475,7 +478,10 @@ __device__ __forceinline__ void walk_rows(const Args& a, const Cache& in, const 
   auto run_of = [&](int pid) {
     return (size_t)((uint32_t)pid < (uint32_t)a.num_pages ? pid : 0) * a.Hkv + kv;
   };
-  auto load = [](const uint8_t* from) {  // (ONCE: no other block reads it)
+  // ONCE: no other block reads it, so it does not push out what others read (64 requests
+  // of 4,096 positions of their own 137 -> 119 us, of 200 to 2,000 over 32,768 shared 114 -> 106; where
+  // all of it stays in the last cache from call to call it costs: 64 of 300 48 -> 50).
+  auto load = [](const uint8_t* from) {
     const u32x4* const p = reinterpret_cast<const u32x4*>(from);
     return ONCE ? __builtin_nontemporal_load(p) : *p;
   };
