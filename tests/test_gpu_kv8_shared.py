@@ -203,6 +203,23 @@ def test_many_items():
     c.check(*c.call())
 
 
+def test_most_requests():
+    """As many requests as a call may have, most of them empty, in groups of one and of three."""
+    rng = np.random.default_rng(13)
+    B = 65535
+    lens = np.zeros(B, int)
+    some = np.sort(rng.permutation(B)[:300])
+    lens[some] = rng.integers(1, 50, 300)
+    lens[-3:] = [20, 30, 17]
+    sizes = [1, 3] * 16383 + [3]
+    b = Batch(rng, 64, 1, 1, 64, 16, False, sizes, [16] * len(sizes), lens.tolist(), 1)
+    out, lse = b.call()
+    b.check(out, lse, only=[0, 1] + some[::4].tolist() + [B - 3, B - 2, B - 1])
+    empty = torch.from_numpy(lens == 0).cuda()
+    assert not out[empty].any() and torch.isneginf(lse[empty]).all()
+    assert torch.isfinite(out).all() and torch.isfinite(lse[~empty]).all()
+
+
 def test_long_line():
     """A prefix that every block takes a piece of, and one long request beside it."""
     rng = np.random.default_rng(9)
