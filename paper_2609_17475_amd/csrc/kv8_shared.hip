@@ -37,9 +37,11 @@ using tiles::walk_tiles;
 constexpr int kRow = 32;        // positions that a wave of the row walk takes at a time (in one page)
 constexpr int kRowWaves = 4, kTileWaves = tiles::kWaves;
 constexpr int kRowThreads = 64 * kRowWaves, kTileThreads = 64 * kTileWaves;
-constexpr int kMinRows = 2;     // rows per wave below which a unit is not cut
-constexpr int kRowCols = 64;    // columns of a group that are walked by rows at most
-constexpr int kSub = 32;        // columns that can have a chunk of their own
+constexpr int kMinRows = 1;     // rows per wave below which a unit is not cut
+// Columns of a group, or left over by its tiles, that the groups' kernel walks by rows at
+// most (32,768 positions, 32/8 heads of 128: with 48 left over rows take 97 us and tiles
+// 91, with 64 94 and 89; 24/4 heads of 256 over 65,536, 64 left over: 105 and 97).
+constexpr int kTileRows = 32;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // What a kernel takes: the groups' shared positions, the requests' own, or both.
@@ -54,8 +56,9 @@ __host__ __device__ constexpr int width_log2(int kind) {
 }
 __host__ __device__ constexpr int width_of(int kind) { return 1 << width_log2(kind); }
 __host__ __device__ constexpr int step_log2(int kind) { return kind >= kTiles1 ? 6 : 5; }
+__host__ __device__ constexpr int rows_of(int cols) { return cols <= 16 ? kRows1 : kRows2; }
 __host__ __device__ constexpr int kind_of(int D, int cols) {
-  return cols <= 16 ? kRows1 : cols <= kRowCols ? kRows2 : cols <= 128 || D > 128 ? kTiles1 : kTiles2;
+  return cols <= kTileRows ? rows_of(cols) : cols <= 128 || D > 128 ? kTiles1 : kTiles2;
 }
 // Cost of a step, and of a unit's start and end, in about 0.1 us of a block.
 __host__ __device__ constexpr int cost_of(int kind) {
@@ -87,11 +90,11 @@ struct Cache {
 };
 struct Args {
   const int32_t *first, *shared;
-  int2* info;     // (first record, records) of each unit: groups', then requests'
+  int2* info;    // (first block, records) of each unit
   int B, G, sq, Hq, Hkv, gq, P, block_shift, num_pages, max_pages;
-  int group_units, own_kind, chunks, own_cols;  // kind, chunks and columns of a request's own units
-  int group_cols;    // columns of a group's record slot
-  int64_t own_recs;  // where requests' records begin (floats; groups' are before)
+  int own_kind;  // of requests' own units
+  int group_gap, own_gap;   // columns from a block's records to the next one's
+  int own_info, own_recs;   // where requests' begin (entries, columns; groups' are before)
   float scale_log2;
   uint32_t flip;  // a negative scale negates the queries instead
 };
@@ -163,10 +166,11 @@ __device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i
     constexpr int W = widest(D);
     const int g = i >> 1;
     t.request = batch.first(g);
-    const int cols = batch.valid ? (batch.first(g + 1) - t.request) * pairs : 0, full = cols & -W;
+    const int cols = batch.valid ? (batch.first(g + 1) - t.request) * pairs : 0;
+    const int full = PART == kBoth ? 0 : cols & -W;
     t.col0 = i & 1 ? full : 0;
     t.cols = i & 1 ? cols : full;
-    t.kind = i & 1 ? kind_of(D, cols - full) : kind_of(D, W);
+    t.kind = PART == kBoth ? rows_of(cols) : kind_of(D, i & 1 ? cols - full : W);
     t.lo = 0, t.hi = t.cols > t.col0 ? batch.shared(g) : 0;
   } else {
     t.request = PART == kOwn ? i : i - 2 * a.G;
@@ -177,20 +181,11 @@ __device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i
   return t;
 }
 
-// A chunk's record slot, its first column there, and its entry of `info`, for a KV head:
-// of a group's columns from `col` on, the group's first request and number given, ..
-template <int D>
-__device__ __forceinline__ void group_place(const Args& a, int request, int g, int col, int kv, int& id,
-                                            int& at, int& entry) {
-  constexpr int W = widest(D);
-  id = (request * a.gq * a.sq / W + g + col / W) * a.Hkv + kv;
-  at = col % W, entry = id * (W / kSub) + at / kSub;
-}
-// .. and of a request's own.
-template <int D>
-__device__ __forceinline__ void own_place(const Args& a, int request, int chunk, int kv, int& id, int& entry) {
-  id = (request * a.chunks + chunk) * a.Hkv + kv;
-  entry = a.group_units * (widest(D) / kSub) + id;
+// Where a chunk of `cols` columns from the request's `col` on has its place for a KV head
+// (counted in columns, one chunk after the other in the line's order): its entry of
+// `info`, and, with a gap of the widest chunk from each block to the next, its records.
+__device__ __forceinline__ int place_of(const Args& a, int request, int col, int cols, int kv) {
+  return (request * a.gq * a.sq + col) * a.Hkv + kv * cols;
 }
 
 // Where a block is on the line: at x, up to end; the window of items that is summed up
@@ -344,18 +339,11 @@ struct Plan {
                                       int records) {
     const int chunk = (int)(((float)u + 0.5f) / (float)g.Hkv), kv = u - chunk * g.Hkv;  // (u below 2^17)
     const int col = it.col0 + (chunk << width_log2(it.kind));
-    int id, first_col, entry;
-    int64_t rec;
-    const int64_t block = blockIdx.x;
-    if (PART == kGroups || (PART == kBoth && i < 2 * g.G)) {
-      group_place<D>(g, it.request, i >> 1, col, kv, id, first_col, entry);
-      rec = ((id + block) * g.group_cols + (first_col & (g.group_cols - 1))) * (D + 4);
-    } else {
-      own_place<D>(g, it.request, chunk, kv, id, entry);
-      rec = g.own_recs + (id + block) * (g.own_cols * (D + 4));
-    }
-    if (r0 == 0 && r1 > 0) g.info[entry] = make_int2(id + blockIdx.x, records);
-    segment = Segment{it, col, kv, r0, r1, rec};
+    const int at = place_of(g, it.request, col, min(width_of(it.kind), it.cols - col), kv);
+    const bool own = PART == kOwn || (PART == kBoth && i >= 2 * g.G);
+    const int64_t rec = (int64_t)(own ? g.own_recs + g.own_gap * blockIdx.x : g.group_gap * blockIdx.x) + at;
+    if (r0 == 0 && r1 > 0) g.info[own ? g.own_info + at : at] = make_int2(blockIdx.x, records);
+    segment = Segment{it, col, kv, r0, r1, rec * (D + 4)};
   }
 
   // All threads: the block's next segment; false: none is left.
@@ -856,7 +844,7 @@ constexpr int kJoinWaves = 4;
 template <int D, bool BF16>
 __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
     const float* __restrict__ recs, const int32_t* __restrict__ lens, uint16_t* __restrict__ out,
-    float* __restrict__ lse, const Args a, int group_blocks, int own_blocks) {
+    float* __restrict__ lse, const Args a, bool both, int group_blocks, int own_blocks) {
   constexpr int kPart = D + 4, kAt = 4;
   __shared__ f32x4 s_num[kJoinWaves][64];
   __shared__ f32x2 s_ml[kJoinWaves][64];
@@ -866,9 +854,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   Batch batch{a.first, a.shared, lens, nullptr, nullptr, nullptr, a.G, a.max_pages * a.P, false, true};
   const int i = blockIdx.x * 64 + lane, pair = min(i / (D / 4), pairs - 1), d4 = i % (D / 4);
   // what does not wait for the groups: the request's own records
-  int id, at, entry;
-  own_place<D>(a, b, pair >> width_log2(a.own_kind), kv, id, entry);
-  const int2 own = a.info[entry];  // (nothing of use where it has none)
+  const int own_width = width_of(a.own_kind), own_col = pair & -own_width;
+  const int own_at = place_of(a, b, own_col, min(own_width, pairs - own_col), kv);
+  const int2 own = a.info[a.own_info + own_at];  // (nothing of use where it has none)
   const int len = batch.length(b);
   int bad = 0;
   for (int i = tid; i <= a.G; i += 64 * kJoinWaves) {
@@ -882,13 +870,13 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
 
   f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
   float M = -INFINITY, den = 0.0f;
-  auto add = [&](const float* from, int64_t stride, int count) {
+  auto add = [&](int from, int gap, int count) {  // (columns)
     for (int r = wave; r < count; r += kJoinWaves * kAt) {
       f32x4 o[kAt];
       f32x2 ml[kAt];
 #pragma unroll
       for (int k = 0; k < kAt; ++k) {
-        const float* p = from + min(r + k * kJoinWaves, count - 1) * stride;
+        const float* p = recs + (int64_t)(from + min(r + k * kJoinWaves, count - 1) * gap) * kPart;
         o[k] = *reinterpret_cast<const f32x4*>(p + 4 * d4);
         ml[k] = *reinterpret_cast<const f32x2*>(p + D);
       }
@@ -909,20 +897,16 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   if (shared > 0) {
     constexpr int W = widest(D);
     const int from = batch.first(group), cols = (batch.first(group + 1) - from) * pairs;
-    const int col = (b - from) * pairs + pair, full = cols & -W, in_full = col < full;
-    const int kind = kind_of(D, in_full ? W : cols - full);
-    const int off = (col - (in_full ? 0 : full)) & (width_of(kind) - 1);  // in its chunk
-    group_place<D>(a, from, group, col - off, kv, id, at, entry);
-    const int2 in = a.info[entry];
-    const int64_t stride = (int64_t)a.group_cols * kPart;
-    add(recs + in.x * stride + (int64_t)((at & (a.group_cols - 1)) + off) * kPart, stride,
-        min(in.y, group_blocks));
+    const int col = (b - from) * pairs + pair, full = both ? 0 : cols & -W;
+    const int begin = col < full ? 0 : full, end = col < full ? full : cols;
+    const int width = width_of(both ? rows_of(cols) : kind_of(D, col < full ? W : cols - full));
+    const int first = begin + ((col - begin) & -width);  // of its chunk
+    const int at = place_of(a, from, first, min(width, end - first), kv);
+    const int2 in = a.info[at];
+    add(at + in.x * a.group_gap + col - first, a.group_gap, min(in.y, group_blocks));
   }
-  if (len > shared) {
-    const int64_t stride = (int64_t)a.own_cols * kPart;
-    add(recs + a.own_recs + own.x * stride + (int64_t)(pair & (width_of(a.own_kind) - 1)) * kPart, stride,
-        min(own.y, own_blocks));
-  }
+  if (len > shared)
+    add(a.own_recs + own_at + own.x * a.own_gap + pair - own_col, a.own_gap, min(own.y, own_blocks));
   s_num[wave][lane] = num;
   s_ml[wave][lane] = f32x2{M, den};
   __syncthreads();
@@ -945,30 +929,40 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   if (lse && d4 == 0) lse[row] = den > 0.0f ? (mx + __log2f(den)) * kLn2 : -INFINITY;
 }
 
-// How the workspace is laid out.
+// How the workspace is laid out: entries, then records.
 struct Layout {
   bool both;  // one kernel for groups and requests
-  int group_blocks, own_blocks, group_units, group_cols, own_kind, chunks, own_cols;
-  int64_t own_recs;
+  int group_blocks, own_blocks, own_kind, group_gap, own_gap, own_info, own_recs;
   size_t recs, bytes;
 };
-Layout layout_of(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq) {
-  const int D = L.head_dim, Hkv = L.num_kv_heads, pairs = Hq / Hkv * sq, W = widest(D);
+Layout layout_of(const jf_kv_layout& L, int32_t B, int32_t sq, int32_t Hq, bool both) {
+  const int D = L.head_dim, pairs = Hq / L.num_kv_heads * sq, columns = B * Hq * sq;
   Layout p;
-  p.both = (int64_t)B * pairs <= kRowCols;  // (no group has more columns)
-  p.own_kind = pairs <= 16 ? kRows1 : kRows2;
-  p.own_blocks = row_blocks(D, !p.both && p.own_kind == kRows1) * num_cus();
-  p.group_blocks = p.both ? p.own_blocks : num_cus();
-  p.group_cols = p.both ? kRowCols : W;
-  p.group_units = (int)(((int64_t)B * pairs / W + G + 1) * Hkv);
-  const int width = width_of(p.own_kind);
-  p.own_cols = std::min(pairs, width);
-  p.chunks = (pairs + width - 1) / width;
-  const int64_t own_units = (int64_t)B * p.chunks * Hkv;
-  p.own_recs = ((int64_t)p.group_units + p.group_blocks) * p.group_cols * (D + 4);
-  p.recs = ((size_t)((int64_t)p.group_units * (W / kSub) + own_units) * sizeof(int2) + 15) / 16 * 16;
-  p.bytes = p.recs + (size_t)(p.own_recs + (own_units + p.own_blocks) * p.own_cols * (D + 4)) * sizeof(float);
+  p.both = both;
+  p.own_kind = rows_of(pairs);
+  p.own_blocks = row_blocks(D, !both && p.own_kind == kRows1) * num_cus();
+  p.group_blocks = both ? p.own_blocks : num_cus();
+  p.group_gap = both ? width_of(kRows2) : widest(D);
+  p.own_gap = std::min(pairs, width_of(p.own_kind));
+  p.own_info = columns;
+  p.own_recs = columns + p.group_blocks * p.group_gap;
+  p.recs = ((size_t)columns * 2 * sizeof(int2) + 15) / 16 * 16;
+  p.bytes = p.recs + (size_t)(p.own_recs + columns + p.own_blocks * p.own_gap) * (D + 4) * sizeof(float);
   return p;
+}
+// Whether rows are walked for groups too, in one kernel with the requests' own positions:
+// for batches of up to 128 columns (rows against tiles, 32/8 heads of 128, 32 requests:
+// over 65,536 positions 70 against 80 us, over 4,096 and 300 of their own 29 against 42;
+// 24/4 heads of 256, 21 requests over 32,768: 53 against 55), and for more where columns,
+// heads and the table's positions are too few to pay for a kernel of tiles, whose records
+// are wider and whose start is longer (64 requests over 4,096: 37 against 58 us, over
+// 16,384: 70 both, over 32,768: 107 against 87; 256 over 4,096: 93 against 96, over 8,192:
+// 135 against 113; heads of 256, 42 requests: over 4,096 35 against 50, over 16,384 62
+// both, over 32,768 97 against 79).
+bool by_rows(const jf_kv_layout& L, int32_t B, int32_t sq, int32_t Hq, int32_t max_pages) {
+  const int64_t columns = (int64_t)B * (Hq / L.num_kv_heads) * sq;
+  const int64_t few = L.head_dim > 128 ? 1 << 24 : 1 << 25;
+  return columns <= 128 || columns * L.num_kv_heads * ((int64_t)max_pages * L.page_size) <= few;
 }
 
 template <int D, bool BF16>
@@ -1000,14 +994,14 @@ hipError_t launch_t(const Cache& in, const int32_t* lens, const Args& a, const L
   const int runs = a.gq * a.sq * (D / 4);
   hipLaunchKernelGGL((kv8_shared_join_kernel<D, BF16>), dim3((runs + 63) / 64, a.Hkv, a.B),
                      dim3(64 * kJoinWaves), 0, stream, recs, lens, static_cast<uint16_t*>(out), lse,
-                     a, p.group_blocks, p.own_blocks);
+                     a, p.both, p.group_blocks, p.own_blocks);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t kv8_shared_bytes(const jf_kv_layout& L, int32_t B, int32_t G, int32_t sq, int32_t Hq) {
-  return layout_of(L, B, G, sq, Hq).bytes;
+size_t kv8_shared_bytes(const jf_kv_layout& L, int32_t B, int32_t, int32_t sq, int32_t Hq) {
+  return std::max(layout_of(L, B, sq, Hq, true).bytes, layout_of(L, B, sq, Hq, false).bytes);
 }
 
 hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
@@ -1016,7 +1010,7 @@ hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
                              const int32_t* group_start, const int32_t* shared_lens, int32_t G,
                              float softmax_scale, void* ws, void* out, float* lse,
                              hipStream_t stream) {
-  const Layout p = layout_of(L, B, G, sq, Hq);
+  const Layout p = layout_of(L, B, sq, Hq, by_rows(L, B, sq, Hq, max_pages));
   int shift = 0;
   while ((1 << shift) < L.group_size) ++shift;
   const Cache in{static_cast<const uint8_t*>(pool.k_codes), static_cast<const uint8_t*>(pool.k_meta),
@@ -1026,7 +1020,8 @@ hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
   a.first = group_start, a.shared = shared_lens, a.info = static_cast<int2*>(ws);
   a.B = B, a.G = G, a.sq = sq, a.Hq = Hq, a.Hkv = L.num_kv_heads, a.gq = Hq / L.num_kv_heads, a.P = L.page_size;
   a.block_shift = shift, a.num_pages = L.num_pages, a.max_pages = max_pages;
-  a.group_units = p.group_units, a.own_kind = p.own_kind, a.chunks = p.chunks, a.own_cols = p.own_cols, a.group_cols = p.group_cols, a.own_recs = p.own_recs;
+  a.own_kind = p.own_kind, a.group_gap = p.group_gap, a.own_gap = p.own_gap;
+  a.own_info = p.own_info, a.own_recs = p.own_recs;
   a.scale_log2 = std::fabs(softmax_scale) * tiles::kLog2e;
   a.flip = softmax_scale < 0.0f ? 0x80008000u : 0u;
   float* const recs = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + p.recs);
