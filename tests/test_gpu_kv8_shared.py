@@ -43,15 +43,23 @@ class Batch:
             self.p.append(k, v, np.cumsum([0] + counts).tolist(), starts, self.tables)
         self.q = rows(rng, B * sq, hq, d, bf16, 0.7).view(B, sq, hq, d)
 
-    def call(self, q=None, scale=None, ws=None, fill=0xFF, **kw):
+    def call(self, q=None, scale=None, ws=None, fill=0xFF, wide_table=False, **kw):
+        """wide_table: as of requests that may grow (another kernel takes the groups then)."""
         q = (self.q if q is None else q).cuda()
+        tables = self.tables
+        if wide_table:
+            P = self.p.lay.page_size
+            tables = np.full((len(tables), 2 ** 25 // (q[..., 0].numel() * P) + 1), -1, np.int32)
+            n = min(self.tables.shape[1], tables.shape[1])
+            tables[:, :n] = self.tables[:, :n]
+            assert n == self.tables.shape[1] or (self.tables[:, n:] < 0).all()
         lay = self.p.lay
         if ws is None:
             n = jfkv.jf_kv8_shared_workspace_bytes(lay, q.shape[0], len(self.shared), self.sq, q.shape[2])
             ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
         out = torch.full_like(q, 7.0)
         lse = torch.full(q.shape[:3], 7.0, device="cuda")
-        jfkv.jf_kv8_shared_attn(self.p.gpu, q, i32(self.tables), i32(self.lens), i32(self.first),
+        jfkv.jf_kv8_shared_attn(self.p.gpu, q, i32(tables), i32(self.lens), i32(self.first),
                                 i32(self.shared), self.scale if scale is None else scale, ws, out,
                                 lse=lse, **kw)
         return out, lse
@@ -119,6 +127,49 @@ def test_shared(P, hkv, hq, d, block, bf16, sizes, shared, lens, sq):
     assert torch.equal(out, no_lse)
 
 
+WIDE = [c for c in CASES if len(c[8]) * c[2] // c[1] * c[9] > 128] + [
+    # columns of full tiles and of what is left over (16, 32, 33, 128, 129), several groups
+    (64, 1, 4, 64, 16, False, [68, 1, 40], [300, 77, 65], [303 + i % 50 for i in range(109)], 1),
+    (64, 2, 16, 128, 32, True, [36], [640], [643 + 5 * i for i in range(36)], 1),
+    (64, 1, 3, 128, 64, False, [11, 32], [130, 64], [140 + 7 * i for i in range(43)], 1),
+    (128, 1, 8, 64, 16, False, [16, 48], [256, 1000], [1001 + i for i in range(64)], 1),
+    (256, 1, 43, 256, 128, True, [3, 1], [700, 0], [701, 900, 702, 90], 3),
+    (64, 2, 6, 256, 16, False, [48], [200], [205 + 3 * i for i in range(48)], 3),
+    (64, 1, 1, 128, 16, True, [129, 2], [90, 100], [91 + i for i in range(131)], 1),
+]
+
+
+@pytest.mark.parametrize("P,hkv,hq,d,block,bf16,sizes,shared,lens,sq", WIDE)
+def test_wide_tables(P, hkv, hq, d, block, bf16, sizes, shared, lens, sq):
+    rng = np.random.default_rng(hq + d + len(lens) + 1)
+    b = Batch(rng, P, hkv, hq, d, block, bf16, sizes, shared, lens, sq)
+    out, lse = b.call(wide_table=True)
+    b.check(out, lse)
+    again, lse2 = b.call(wide_table=True, fill=0x55)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    b.check(*b.call())
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_wide_tables_where_it_goes_wrong(d):
+    """Short and empty requests, no requests' own positions, pages outside the pool, bounds that
+    do not ascend, negative scales: with tiles."""
+    rng = np.random.default_rng(d)
+    lens = [400] + [int(x) for x in rng.integers(0, 700, 79)]
+    lens[5:9] = [0, 399, 400, 401]
+    b = Batch(rng, 64, 1, 4, d, 16, d == 128, [80], [400], lens, 1)
+    b.check(*b.call(wide_table=True))
+    b.check(*b.call(wide_table=True, scale=-0.2), scale=-0.2)
+    c = Batch(rng, 64, 1, 4, d, 16, d == 128, [80], [256], [256] * 80, 1)
+    c.check(*c.call(wide_table=True))
+    c.tables[0, 2] = len(c.p.host.pool_bytes()[0])  # (beyond any page)
+    c.check(*c.call(wide_table=True))
+    b.first, b.cut = [0, 81], [0] * 80  # every request by itself
+    b.tables[1:, :7] = b.tables[0, :7]
+    b.lens = [min(n, 400) for n in b.lens]
+    b.check(*b.call(wide_table=True))
+
+
 @pytest.mark.parametrize("sq", [1, 3])
 def test_lengths_on_either_side_of_the_shared_positions(sq):
     """Requests that end before, at and just behind them, or hold nothing; groups of one, of
@@ -181,12 +232,14 @@ def test_where_exponents_jump(d, bf16, count):
     v = (rows(rng, n, 1, d, False).double() * torch.from_numpy(size)).to(dtype_of(bf16))
     b.p.append(k, v, [0, n], [0], b.tables[:1])
     b.check(*b.call())
+    b.check(*b.call(wide_table=True))
     v[:] = v.abs() + 1  # and a needle: all weight on a position whose values are the smallest
     v[100:104] = 2.0 ** -12
     k[100] = 8.0
     b.p.append(k, v, [0, n], [0], b.tables[:1])
     b.q[:] = 1.0
     b.check(*b.call())
+    b.check(*b.call(wide_table=True))
 
 
 def test_many_items():
@@ -198,9 +251,11 @@ def test_many_items():
     lens = [int(n) if rng.random() < 0.3 else 0 for n in rng.integers(0, 60, B)]
     b = Batch(rng, 64, 1, 1, 64, 16, False, sizes, shared, lens, 1)
     b.check(*b.call())
+    b.check(*b.call(wide_table=True))
     sizes, shared = [B], [0]  # one group, nothing shared
     c = Batch(rng, 64, 1, 2, 64, 16, True, sizes, shared, lens, 1)
     c.check(*c.call())
+    c.check(*c.call(wide_table=True))
 
 
 def test_most_requests():
@@ -213,11 +268,12 @@ def test_most_requests():
     lens[-3:] = [20, 30, 17]
     sizes = [1, 3] * 16383 + [3]
     b = Batch(rng, 64, 1, 1, 64, 16, False, sizes, [16] * len(sizes), lens.tolist(), 1)
-    out, lse = b.call()
-    b.check(out, lse, only=[0, 1] + some[::4].tolist() + [B - 3, B - 2, B - 1])
     empty = torch.from_numpy(lens == 0).cuda()
-    assert not out[empty].any() and torch.isneginf(lse[empty]).all()
-    assert torch.isfinite(out).all() and torch.isfinite(lse[~empty]).all()
+    for wide_table in (False, True):
+        out, lse = b.call(wide_table=wide_table)
+        b.check(out, lse, only=[0, 1] + some[::4].tolist() + [B - 3, B - 2, B - 1])
+        assert not out[empty].any() and torch.isneginf(lse[empty]).all()
+        assert torch.isfinite(out).all() and torch.isfinite(lse[~empty]).all()
 
 
 def test_long_line():
