@@ -1,7 +1,14 @@
-// The chunk attention's walk over tiles of 64 positions (format: jfkv_kv8.h): a block of
-// eight waves, each with column sets of its own, over one KV head.  Shared by the
-// attention of a chunk and of requests that share prefixes; kv8_prefill.hip says what
-// bounds it.
+// A walk over tiles of 64 positions (format: jfkv_kv8.h) of one KV head: a block of eight
+// waves, each with column sets of its own, all of which see the same positions but for
+// what `Sees` hides.  It is the chunk attention's (kv8_prefill.hip says what bounds it)
+// with an order of its own within a turn; that kernel, whose causal masks end each
+// block elsewhere, keeps its own text: with this one it took 2-7 % longer.
+//
+// A turn of 64 positions, 256 columns and d = 128 takes some 4,900 cycles: the products
+// 1,700 (1,024 of matrix cores, 1,024 of LDS reads for four waves), the softmax 1,800
+// (32 exponentials at a quarter of the rate and some 100 vector instructions), the next
+// tiles' way into LDS 700-900.  Two waves of a SIMD take products and softmax in turns.
+// 1,024 columns over 65,536 positions: 300-322 us, 850-920 TFLOP/s.
 #pragma once
 
 #include <type_traits>
@@ -69,10 +76,7 @@ __device__ __forceinline__ void walk_tiles(
   auto page_of = [&](const Place& at) JF_INLINE { return table[min(at.page, last_page)]; };
   // A tile without a page in the pool travels as page 0's, but counts as a tile of
   // zeros that nobody sees: page 0's codes may be NaN and its exponents are someone
-  // else's.  (Its values are cleared by a mask on every tile.  Times against none at
-  // all, 2,048 rows over 65,536 positions and, d = 256, 256 over 196,608: 0.96 and
-  // 0.99; with a branch around the mask 1.00 and 1.02, around the products instead
-  // 1.01 and 1.00.)
+  // else's.  (Its values are cleared by a mask on every tile: a branch costs more.)
   auto held = [&](int pid) JF_INLINE { return (uint32_t)pid < (uint32_t)num_pages; };
   // (pages times heads are below 2^31)
   auto run_of = [&](int pid) JF_INLINE { return (uint32_t)(held(pid) ? pid : 0) * (uint32_t)Hkv + (uint32_t)kv; };
@@ -232,9 +236,9 @@ __device__ __forceinline__ void walk_tiles(
 
   // The products of turn j: the values of tile j - 1, then the scores of tile j.  Their
   // operands are one run in LDS, each read kAhead before its products, so that a turn
-  // waits for the first of them only once (as three runs: 2.65 against XX us a tile at
-  // d = 128).  (The barriers keep the compiler from reading all of them at once, which
-  // spills.)
+  // waits for the first of them only once.  (The barriers keep the compiler from reading
+  // all of them at once, which spills; with two sets of columns or d = 256 eight ahead
+  // spill too.)
   constexpr int kAhead = NC == 1 && D <= 128 ? 8 : 4, kV = 8 * C, kAll = 16 * C;
   auto products = [&](int j) JF_INLINE {
     const u32x4* const from = lds + (j & 1 ? 2 : 0) * kTileSize + lane;
@@ -304,11 +308,12 @@ __device__ __forceinline__ void walk_tiles(
 
   // ---- Turn j forms the scores of tile j and the value products of tile j - 1.
   // Waves w and w + 4 share a SIMD: the first do their matrix products at once and
-  // the vector work (the softmax, the next tiles' way into LDS) after them, the
-  // second the other way round, so that one's matrix products meet the other's
-  // vector work (d = 256: 256 rows over 196,608 positions 1,790 -> 1,430 us; at d =
-  // 64, where the vector work is the most, all do the same).  (Two loops, as one loop
-  // with both orders spills; every wave passes j1 - j0 + 1 barriers in either.)
+  // the softmax after them, the second the other way round, so that one's matrix
+  // products meet the other's vector work; both carry the next tiles last (between the
+  // two, as the chunk attention does: 1,024 columns over 65,536 positions 361 us against
+  // 322, 256 columns 117 against 108).  At d = 64, where the vector work is the most, all
+  // do the same.  (Two loops, as one loop with both orders spills; every wave passes
+  // j1 - j0 + 1 barriers in either.)
   auto walk = [&](auto is_late) JF_INLINE {
     constexpr bool late = decltype(is_late)::value;
     Place at = {j0 * kTile / P, j0 * kTile % P};

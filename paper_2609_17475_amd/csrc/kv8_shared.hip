@@ -10,14 +10,23 @@
 //
 // The (request, token, head) triples that read a KV head are the columns of the
 // matrix products, 16 to a set, and what kv8_decode.hip says of operands, exponents
-// and roundings holds here too.  Two kernels: one walks rows of 32 positions, each wave
-// its own (requests' own positions, groups of few columns; bound by HBM), one walks
-// tiles of 64 positions, each wave with columns of its own (groups of many columns;
+// and roundings holds here too.  Two ways to walk: rows of 32 positions, each wave its
+// own for up to 32 columns (requests' own positions, small groups; bound by HBM, or by
+// latency), and tiles of 64 positions, each wave with columns of its own (large groups;
 // bound by the vector work beside the matrix cores, as the chunk attention).  The work
-// of either is a line of units: for each group its chunks of columns and KV heads, then
-// for each request its KV heads; a unit is a run of steps over positions.  The line is
-// cut into pieces of equal cost, a block each, wherever that falls; each (block, unit)
-// leaves one record, which a last launch joins.
+// of a launch is a line of units: for each group its chunks of columns and KV heads,
+// then for each request its KV heads; a unit is a run of steps over positions.  The
+// line is cut into pieces of equal cost, a block each, wherever that falls; each
+// (block, unit) leaves one record, which a last launch joins.  Small batches have one
+// kernel before that, large ones a kernel of tiles and one of rows (the registers that
+// tiles need leave rows too few waves: 256 requests of 300 positions over 256 shared
+// 79 us in one kernel of both, 72 in two).
+//
+// A step of 64 requests of 200 to 2,000 positions over 32,768 shared (32/8 heads of
+// 128) takes 106 us: 59 in the tiles (half of it vector work and matrix products, the
+// rest the plan, queries, first tiles, and 35 MB of records), 38 in the rows (4 TB/s),
+// 9 in the join; 256 requests over 65,536 350 us, 300 of them in the tiles, 920 TFLOP/s;
+// two requests over 4,096 14 us: a plan, a walk and a join, each a chain of latencies.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -37,7 +46,7 @@ using tiles::walk_tiles;
 constexpr int kRow = 32;        // positions that a wave of the row walk takes at a time (in one page)
 constexpr int kRowWaves = 4, kTileWaves = tiles::kWaves;
 constexpr int kRowThreads = 64 * kRowWaves, kTileThreads = 64 * kTileWaves;
-constexpr int kMinRows = 1;     // rows per wave below which a unit is not cut
+constexpr int kMinRows = 1;     // rows per wave below which a unit is not cut (1: 14.2 us, 2: 14.7, 4: 16.0)
 // Columns of a group, or left over by its tiles, that the groups' kernel walks by rows at
 // most (32,768 positions, 32/8 heads of 128: with 48 left over rows take 97 us and tiles
 // 91, with 64 94 and 89; 24/4 heads of 256 over 65,536, 64 left over: 105 and 97).
@@ -48,7 +57,10 @@ constexpr float kLn2 = 0.69314718055994530942f;
 enum Part { kGroups, kOwn, kBoth };
 
 // How a chunk of columns is computed: by rows, one or two sets of 16 columns for all of
-// a block's waves, or by tiles, one or two sets for each of eight waves.
+// a block's waves, or by tiles, one or two sets for each of eight waves.  (One set beside
+// two: each LDS operand feeds two products; at d = 128, 256 columns over 65,536 positions
+// 105 us against 126 in chunks of 128, 1,024 columns 322 against 419.  At d = 256 two
+// sets do not fit into the registers.)
 enum Kind { kRows1, kRows2, kTiles1, kTiles2 };
 __host__ __device__ constexpr int widest(int D) { return D > 128 ? 128 : 256; }
 __host__ __device__ constexpr int width_log2(int kind) {
@@ -60,7 +72,9 @@ __host__ __device__ constexpr int rows_of(int cols) { return cols <= 16 ? kRows1
 __host__ __device__ constexpr int kind_of(int D, int cols) {
   return cols <= kTileRows ? rows_of(cols) : cols <= 128 || D > 128 ? kTiles1 : kTiles2;
 }
-// Cost of a step, and of a unit's start and end, in about 0.1 us of a block.
+// Cost of a step, and of a unit's start and end, in about 0.1 us of a block.  (Half or
+// twice the start: 64 requests of 60 positions 37 -> 41 and 37 us, of 4,096 117 -> 118 and
+// 120.)
 __host__ __device__ constexpr int cost_of(int kind) {
   return kind == kRows1 ? 4 : kind == kRows2 ? 5 : kind == kTiles1 ? 16 : 24;
 }
@@ -204,8 +218,10 @@ struct Segment {
 // The plan of a block of T threads: which segments it has.  Where units are few, each is
 // cut into equal shares, as many for all units as there are blocks, and a block has one
 // share; else the units follow one another on a line, each with its start's cost, and
-// the line is cut into pieces of one length.  (What lives from one segment to the next
-// is in LDS, so that the walks have the registers.)
+// the line is cut into pieces of one length.  (Two requests over 4,096 positions: 14.7 us
+// in shares, 16.7 on the line, where a piece may begin in one unit and end in the next;
+// 16 over 8,192: 24.3 and 30.3; four groups of 24: 108 and 115.  What lives from one
+// segment to the next is in LDS, so that the walks have the registers.)
 template <int T>
 struct Plan {
   static constexpr int kTeams = T / 64;

@@ -18,7 +18,8 @@ constexpr int kThreads = 256;
 // in 64 bits, as an angle of a far position has lost its place on the circle in 32:
 // the product with its rounding error (exact together), less k quarter turns
 // (pi / 2 as a sum of two numbers), then the Taylor series on [-pi/4, pi/4], whose
-// next terms are below 2^-37.
+// next terms are below 2^-37.  65,537 positions of 64 pairs: 15-16 us for 34 MB; a step's
+// few rows 1.6 us, a launch.
 __global__ __launch_bounds__(kThreads) void rope_table_kernel(
     const int32_t* __restrict__ positions, const float* __restrict__ freq, float* __restrict__ table,
     int half, int64_t n, float magnitude) {
@@ -57,7 +58,12 @@ struct Rows {
   int heads;
 };
 
-// A wave takes a run of the items of one token's heads, q's before k's.
+// A wave takes a run of the items of one token's heads, q's before k's; lanes 64 items on
+// meet the same pairs of another head where 64 is a multiple of a head's items, and keep
+// their angles then.  HBM-bound: every element read and written once, 16 bytes a lane (in
+// place, only the rotated dims).  65,537 tokens of 32 + 8 heads of 128: 255 us and the
+// table's 16, 5.2 TB/s, a copy's rate; 8,192 of 24 + 4 heads of 256 out of a projection's
+// rows of 32 heads 51 us, 4.6 TB/s; eight tokens 3.4 us, a launch and two loads in a row.
 template <int V, bool BF16, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rope_rotate_kernel(
     const float* __restrict__ table, const int32_t* __restrict__ rows, int table_rows, int half,
