@@ -62,12 +62,20 @@ struct Turn {
   const uint16_t* q;
   uint16_t* q_out;
   int q_heads;
+  bool together;
 };
 struct NoTurn {};
 
+// The grid's x is a multiple of the XCDs, so that a block of tokens has all of its heads
+// on one of them.  A table that outgrows an XCD's L2 (4 MB) is also read by all heads and
+// parts of a block of tokens one after the other: 65,535 rows, 34 MB of angles, 326 -> 319
+// us; 2,048 rows, 0.5 MB, would take 16.6 us for 15.1.
+constexpr uint32_t kXcds = 8;
+constexpr int64_t kTableTogether = 4 << 20;
+
 // 8 dims of a row of head_dim D, from dim `base` on, rotated; the partner dims are
 // read from the row as well (they are another lane's, in the first-level cache).  65,535
-// rows of 8 heads of 128 and 32 of queries: 327 us, 4.6 TB/s in and out of HBM; a row of
+// rows of 8 heads of 128 and 32 of queries: 318 us, 4.7 TB/s in and out of HBM; a row of
 // each of eight requests 5.8 us, as without rotation.
 template <bool BF16>
 __device__ __forceinline__ void turn8(uint32_t (&raw)[4], const uint16_t* x, const float* angles,
@@ -101,13 +109,15 @@ __device__ __forceinline__ void turn8(uint32_t (&raw)[4], const uint16_t* x, con
   }
 }
 
-// The rows of queries, a token's heads by a block at a time.
+// The rows of queries, a token's heads by a block at a time: unit of units takes a run of
+// tokens, block h of its `heads` every `heads`-th of them.
 template <bool BF16, bool PAIRS>
-__device__ __forceinline__ void turn_queries(const Turn& r, int D, int64_t block, int64_t blocks,
+__device__ __forceinline__ void turn_queries(const Turn& r, int D, int unit, int units, int h, int heads,
                                              int total) {
   using namespace rope;
   const int items = D / 16, n_rot = r.half / 8;
-  for (int64_t t = block; t < total; t += blocks) {
+  const int64_t run = (total + (int64_t)units - 1) / units, end = min((unit + 1) * run, (int64_t)total);
+  for (int64_t t = unit * run + h; t < end; t += heads) {
     const float* const angles = r.table + row_of(r.rows, r.table_rows, t) * (2 * (int64_t)r.half);
     for (int i = threadIdx.x; i < r.q_heads * items; i += blockDim.x) {
       const int item = i % items, at = i / items * D;
@@ -144,23 +154,27 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
   constexpr uint32_t kInf = BF16 ? 0x7f80u : 0x7c00u;  // magnitudes from here on are not finite
   __shared__ uint32_t s_max[4];
   const int tid = threadIdx.x, lane = tid & 63, nthr = blockDim.x;
-  const int h = blockIdx.y;
-  const bool is_v = blockIdx.z != 0;
+  int unit = blockIdx.x, h = blockIdx.y, part = blockIdx.z;
   const int64_t cap = (int64_t)max_pages * P;
   if constexpr (ROPE) {
-    if (blockIdx.z == 2) {
-      const int64_t units = (int64_t)gridDim.x * gridDim.y;
-      const int64_t unit = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    if (rope.together) {
+      const uint32_t parts = gridDim.y * gridDim.z;
+      const uint32_t at = unit + gridDim.x * (h + gridDim.y * part), slot = at / kXcds;
+      unit = slot / parts * kXcds + at % kXcds;
+      h = slot % parts % gridDim.y, part = slot % parts / gridDim.y;
+    }
+    if (part == 2) {
       if (rope.pairs)
-        turn_queries<BF16, true>(rope, D, unit, units, total);
+        turn_queries<BF16, true>(rope, D, unit, gridDim.x, h, gridDim.y, total);
       else
-        turn_queries<BF16, false>(rope, D, unit, units, total);
+        turn_queries<BF16, false>(rope, D, unit, gridDim.x, h, gridDim.y, total);
       return;
     }
   }
+  const bool is_v = part != 0;
 
   // ---- the request and block of this unit: every wave scans the block counts
-  int u = blockIdx.x, b = 0;
+  int u = unit, b = 0;
   Span sp;
   if (B == 1) {
     sp = span_of(cu, start, 0, total, cap, block);
@@ -333,7 +347,8 @@ hipError_t launch_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, boo
   const int threads = std::min(items, 256);
   // blocks that total_tok rows of B requests can touch: one per row at most,
   // and whole blocks plus two partial ones per request
-  const int64_t units = std::min<int64_t>(total_tok, total_tok / block + 2 * (int64_t)B);
+  int64_t units = std::min<int64_t>(total_tok, total_tok / block + 2 * (int64_t)B);
+  if (ROPE) units = (units + kXcds - 1) / kXcds * kXcds;
   const dim3 grid((uint32_t)units, L.num_kv_heads, parts);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<uint8_t*>(pool.k_codes),
@@ -369,7 +384,7 @@ hipError_t launch_kv8_rope_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& 
                                   int32_t max_pages, int32_t total_tok, hipStream_t stream) {
   const Turn turn{r.table, r.rows, r.table_rows, r.rot_dim / 2, r.order == JF_ROPE_PAIRS,
                   k_stride, v_stride, q_stride, static_cast<const uint16_t*>(q),
-                  static_cast<uint16_t*>(q_out), Hq};
+                  static_cast<uint16_t*>(q_out), Hq, (int64_t)total_tok * r.rot_dim * 4 > kTableTogether};
   return launch_append<true>(L, pool, bf16, k_new, v_new, cu_tok, start_pos, block_tables, B,
                              max_pages, total_tok, turn, q ? 3 : 2, stream);
 }

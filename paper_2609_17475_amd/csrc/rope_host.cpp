@@ -177,7 +177,7 @@ jf_status jf_kv8_rope_append(const jf_kv_layout* layout, const jf_kv_pool_ptrs* 
     if (q == q_out && total_tok > 1 && q_stride != q_row)
       return fail(JF_ERR_INVALID, "q in place must have no gaps");
   }
-  if (((int64_t)total_tok / layout->group_size + 2 * (int64_t)B) * 256 > kMaxThreads)
+  if (((int64_t)total_tok / layout->group_size + 2 * (int64_t)B + 7) * 256 > kMaxThreads)
     return fail(JF_ERR_UNSUPPORTED, "total_tok %d too large for one launch", total_tok);
   return device_status(jfkv::launch_kv8_rope_append(*layout, *pool, dtype == JF_BF16, *rope, k_new,
                                                     k_stride, v_new, v_stride, q, q_stride, q_out,
