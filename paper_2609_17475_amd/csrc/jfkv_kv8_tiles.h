@@ -80,7 +80,9 @@ __device__ __forceinline__ void walk_tiles(
   auto held = [&](int pid) JF_INLINE { return (uint32_t)pid < (uint32_t)num_pages; };
   // (pages times heads are below 2^31)
   auto run_of = [&](int pid) JF_INLINE { return (uint32_t)(held(pid) ? pid : 0) * (uint32_t)Hkv + (uint32_t)kv; };
-  auto place = [&](int slot0, int pid) JF_INLINE { return ((uint64_t)run_of(pid) * (uint32_t)P + (uint32_t)slot0) * D; };
+  auto place = [&](int slot0, int pid) JF_INLINE {
+    return ((uint64_t)run_of(pid) * (uint32_t)P + (uint32_t)slot0) * D;
+  };
   const uint32_t k_off = (tid % kOf / D * 16 + (lane & 15)) * D + tid % D / 64 * 64 + (lane >> 4) * 16;
   auto fetch_k = [&](int slot0, int pid) JF_INLINE {
     const uint8_t* kp = k_codes + place(slot0, pid);

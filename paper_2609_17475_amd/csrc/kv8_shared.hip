@@ -57,10 +57,10 @@ constexpr float kLn2 = 0.69314718055994530942f;
 enum Part { kGroups, kOwn, kBoth };
 
 // How a chunk of columns is computed: by rows, one or two sets of 16 columns for all of
-// a block's waves, or by tiles, one or two sets for each of eight waves.  (One set beside
-// two: each LDS operand feeds two products; at d = 128, 256 columns over 65,536 positions
-// 105 us against 126 in chunks of 128, 1,024 columns 322 against 419.  At d = 256 two
-// sets do not fit into the registers.)
+// a block's waves, or by tiles, one or two sets for each of eight waves.  (With
+// two each LDS operand feeds two products: at d = 128, 256 columns over 65,536 positions
+// take 105 us, with one set 126, 1,024 columns 322 and 419.  At d = 256 two do not fit
+// into the registers.)
 enum Kind { kRows1, kRows2, kTiles1, kTiles2 };
 __host__ __device__ constexpr int widest(int D) { return D > 128 ? 128 : 256; }
 __host__ __device__ constexpr int width_log2(int kind) {
@@ -444,8 +444,8 @@ struct Row {
 
 // What column `col` of an item's request reads: its query, and how many positions.
 template <int D>
-__device__ __forceinline__ const uint16_t* query_of(const Args& a, const Cache& in, const Batch& batch, const Item& it,
-                                                    int col, int kv, int& see) {
+__device__ __forceinline__ const uint16_t* query_of(const Args& a, const Cache& in, const Batch& batch,
+                                                    const Item& it, int col, int kv, int& see) {
   const int row = col / a.gq;
   see = min(batch.length(it.request + row / a.sq) - a.sq + 1 + row % a.sq, it.hi);
   return in.q + (((size_t)it.request * a.sq + row) * a.Hq + kv * a.gq + col % a.gq) * D;
@@ -874,15 +874,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   const int own_at = place_of(a, b, own_col, min(own_width, pairs - own_col), kv);
   const int2 own = a.info[a.own_info + own_at];  // (nothing of use where it has none)
   const int len = batch.length(b);
-  int bad = 0;
-  for (int i = tid; i <= a.G; i += 64 * kJoinWaves) {
-    const int at = a.first[i];
-    bad |= i == 0 ? at != 0 : at < a.first[i - 1];
-    if (i == a.G) bad |= at != a.B;
+  int group, from, to, shared;  // the request's group, its requests and shared positions
+  if (a.G < 64) {       // a lane for each bound: two loads in a row less (16 requests over 8,192 positions 23.8 -> 23.5 us)
+    const int at = lane <= a.G ? a.first[lane] : 0, before = __shfl_up(at, 1);
+    const int most = lane < a.G ? a.shared[lane] : 0;
+    batch.valid = !__any(lane <= a.G && (lane == 0 ? at != 0 : at < before || (lane == a.G && at != a.B)));
+    group = max(__popcll(__ballot(lane < a.G && at <= b)) - 1, 0);
+    from = __builtin_amdgcn_readlane(at, group), to = __builtin_amdgcn_readlane(at, group + 1);
+    const int first_most = __builtin_amdgcn_readlane(most, group);
+    shared = batch.valid && to - from > 1 ? min(max(first_most, 0), batch.length(from)) : 0;
+  } else {
+    int bad = 0;
+    for (int i = tid; i <= a.G; i += 64 * kJoinWaves) {
+      const int at = a.first[i];
+      bad |= i == 0 ? at != 0 : at < a.first[i - 1];
+      if (i == a.G) bad |= at != a.B;
+    }
+    batch.valid = !__syncthreads_or(bad);
+    group = batch.valid ? batch.of(b) : 0;
+    from = batch.first(group), to = batch.first(group + 1);
+    shared = batch.shared(group);
   }
-  batch.valid = !__syncthreads_or(bad);
-  const int group = batch.valid ? batch.of(b) : 0;
-  const int shared = batch.valid ? batch.shared(group) : 0;
 
   f32x4 num = {0.0f, 0.0f, 0.0f, 0.0f};
   float M = -INFINITY, den = 0.0f;
@@ -912,7 +924,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   };
   if (shared > 0) {
     constexpr int W = widest(D);
-    const int from = batch.first(group), cols = (batch.first(group + 1) - from) * pairs;
+    const int cols = (to - from) * pairs;
     const int col = (b - from) * pairs + pair, full = both ? 0 : cols & -W;
     const int begin = col < full ? 0 : full, end = col < full ? full : cols;
     const int width = width_of(both ? rows_of(cols) : kind_of(D, col < full ? W : cols - full));
