@@ -1203,6 +1203,8 @@ def _rope_type(*tensors) -> int:
     """JF_ type of rows (all the same), their device checked."""
     import torch
     given = [(t, name) for t, name in tensors if t is not None]
+    if not given:
+        raise ValueError("no rows are given")
     dtype = given[0][0].dtype
     if dtype not in (torch.float16, torch.bfloat16):
         raise ValueError("%s must be float16 or bfloat16, got %s" % (given[0][1], dtype))

@@ -2,9 +2,11 @@
 launched)."""
 import ctypes
 import math
+import types
 
 import numpy as np
 import pytest
+import torch
 
 jfkv = pytest.importorskip("paper_2609_17475_amd.jfkv")
 L = jfkv.lib
@@ -149,3 +151,11 @@ def test_frequency_arguments():
     assert call(factor=-1.0, length=-5, fast=0.0) == OK  # what plain frequencies do not use
     with pytest.raises(ValueError):
         jfkv.rope_frequencies(64, scaling="none")
+
+
+def test_rows_of_the_binding():
+    table = types.SimpleNamespace(table=None, rows=None)  # (looked at after the rows)
+    x = torch.zeros(2, 1, 16, dtype=torch.float16)
+    for q, q_out in ((None, None), (x, x), (x.float(), x.float())):  # none, on the host, fp32
+        with pytest.raises(ValueError):
+            jfkv.bind_rope_rotate(table, q, q_out)
