@@ -66,16 +66,16 @@ struct Turn {
 };
 struct NoTurn {};
 
-// The grid's x is a multiple of the XCDs, so that a block of tokens has all of its heads
-// on one of them.  A table that outgrows an XCD's L2 (4 MB) is also read by all heads and
-// parts of a block of tokens one after the other: 65,535 rows, 34 MB of angles, 326 -> 319
-// us; 2,048 rows, 0.5 MB, would take 16.6 us for 15.1.
+// A table that outgrows an XCD's L2 (4 MB) is read by all heads and parts of a block of
+// tokens one after the other on one XCD: 65,535 rows, 34 MB of angles, 327 -> 318 us, 848
+// MB read for 1,133.  (Few blocks would be shared out unevenly: 2,048 rows, 0.5 MB, take
+// 15.4 us in the grid's order, 15.0 to 16.9 with a block's heads on one XCD.)
 constexpr uint32_t kXcds = 8;
 constexpr int64_t kTableTogether = 4 << 20;
 
 // 8 dims of a row of head_dim D, from dim `base` on, rotated; the partner dims are
 // read from the row as well (they are another lane's, in the first-level cache).  65,535
-// rows of 8 heads of 128 and 32 of queries: 318 us, 4.7 TB/s in and out of HBM; a row of
+// rows of 8 heads of 128 and 32 of queries: 313-319 us, 4.7-4.8 TB/s in and out of HBM; a row of
 // each of eight requests 5.8 us, as without rotation.
 template <bool BF16>
 __device__ __forceinline__ void turn8(uint32_t (&raw)[4], const uint16_t* x, const float* angles,
@@ -109,15 +109,18 @@ __device__ __forceinline__ void turn8(uint32_t (&raw)[4], const uint16_t* x, con
   }
 }
 
-// The rows of queries, a token's heads by a block at a time: unit of units takes a run of
-// tokens, block h of its `heads` every `heads`-th of them.
+// The rows of queries, a token's heads by a block at a time: together, a unit takes a run
+// of tokens and block h of its `heads` every `heads`-th of them; else all blocks take
+// turns.
 template <bool BF16, bool PAIRS>
 __device__ __forceinline__ void turn_queries(const Turn& r, int D, int unit, int units, int h, int heads,
                                              int total) {
   using namespace rope;
   const int items = D / 16, n_rot = r.half / 8;
-  const int64_t run = (total + (int64_t)units - 1) / units, end = min((unit + 1) * run, (int64_t)total);
-  for (int64_t t = unit * run + h; t < end; t += heads) {
+  const int64_t run = (total + (int64_t)units - 1) / units;
+  const int64_t end = r.together ? min((unit + 1) * run, (int64_t)total) : total;
+  const int64_t step = r.together ? heads : (int64_t)heads * units;
+  for (int64_t t = r.together ? unit * run + h : h * (int64_t)units + unit; t < end; t += step) {
     const float* const angles = r.table + row_of(r.rows, r.table_rows, t) * (2 * (int64_t)r.half);
     for (int i = threadIdx.x; i < r.q_heads * items; i += blockDim.x) {
       const int item = i % items, at = i / items * D;
@@ -348,7 +351,8 @@ hipError_t launch_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, boo
   // blocks that total_tok rows of B requests can touch: one per row at most,
   // and whole blocks plus two partial ones per request
   int64_t units = std::min<int64_t>(total_tok, total_tok / block + 2 * (int64_t)B);
-  if (ROPE) units = (units + kXcds - 1) / kXcds * kXcds;
+  if constexpr (ROPE)
+    if (rope.together) units = (units + kXcds - 1) / kXcds * kXcds;
   const dim3 grid((uint32_t)units, L.num_kv_heads, parts);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<uint8_t*>(pool.k_codes),
