@@ -34,60 +34,21 @@
 
 #include "jfkv_internal.h"
 #include "jfkv_kv8.h"
+#include "jfkv_kv8_shared_plan.h"
 #include "jfkv_kv8_tiles.h"
 
 namespace jfkv {
 namespace {
 
 using namespace kv8;
+using namespace kv8::shared;
 using tiles::kTile;
 using tiles::walk_tiles;
 
 constexpr int kRow = 32;        // positions that a wave of the row walk takes at a time (in one page)
-constexpr int kRowWaves = 4, kTileWaves = tiles::kWaves;
+constexpr int kTileWaves = tiles::kWaves;
 constexpr int kRowThreads = 64 * kRowWaves, kTileThreads = 64 * kTileWaves;
-constexpr int kMinRows = 1;     // rows per wave below which a unit is not cut (1: 14.2 us, 2: 14.7, 4: 16.0)
-// Columns of a group, or left over by its tiles, that the groups' kernel walks by rows at
-// most (32,768 positions, 32/8 heads of 128: with 48 left over rows take 97 us and tiles
-// 91, with 64 94 and 89; 24/4 heads of 256 over 65,536, 64 left over: 105 and 97).
-constexpr int kTileRows = 32;
 constexpr float kLn2 = 0.69314718055994530942f;
-
-// What a kernel takes: the groups' shared positions, the requests' own, or both.
-enum Part { kGroups, kOwn, kBoth };
-
-// How a chunk of columns is computed: by rows, one or two sets of 16 columns for all of
-// a block's waves, or by tiles, one or two sets for each of eight waves.  (With
-// two each LDS operand feeds two products: at d = 128, 256 columns over 65,536 positions
-// take 105 us, with one set 126, 1,024 columns 322 and 419.  At d = 256 two do not fit
-// into the registers.)
-enum Kind { kRows1, kRows2, kTiles1, kTiles2 };
-__host__ __device__ constexpr int widest(int D) { return D > 128 ? 128 : 256; }
-__host__ __device__ constexpr int width_log2(int kind) {
-  return kind == kRows1 ? 4 : kind == kRows2 ? 5 : kind == kTiles1 ? 7 : 8;
-}
-__host__ __device__ constexpr int width_of(int kind) { return 1 << width_log2(kind); }
-__host__ __device__ constexpr int step_log2(int kind) { return kind >= kTiles1 ? 6 : 5; }
-__host__ __device__ constexpr int rows_of(int cols) { return cols <= 16 ? kRows1 : kRows2; }
-__host__ __device__ constexpr int kind_of(int D, int cols) {
-  return cols <= kTileRows ? rows_of(cols) : cols <= 128 || D > 128 ? kTiles1 : kTiles2;
-}
-// Cost of a step, and of a unit's start and end, in about 0.1 us of a block.  (Half or
-// twice the start: 64 requests of 60 positions 37 -> 41 and 37 us, of 4,096 117 -> 118 and
-// 120.)
-__host__ __device__ constexpr int cost_of(int kind) {
-  return kind == kRows1 ? 4 : kind == kRows2 ? 5 : kind == kTiles1 ? 16 : 24;
-}
-__host__ __device__ constexpr int start_of(int kind) { return kind >= kTiles1 ? 60 : 30; }
-
-// Blocks of the row walk per CU.  One set of columns leaves room for more, which hides
-// more of a unit's start (three in place of two, 32/8 heads of 128: 256 requests of 300
-// positions of their own 79 -> 72 us, 64 of 300 40 -> 37; 64 of 4,096 133 -> 137).  A
-// kernel that takes groups as well has two: its second walk would spill (16 requests over
-// 8,192 shared positions 24.2 -> 26.9 us with three).
-__host__ __device__ constexpr int row_blocks(int D, bool one_set) {
-  return one_set ? (D > 128 ? 2 : D > 64 ? 3 : 4) : 2;
-}
 
 // Values that are the same in all lanes, to scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -112,13 +73,6 @@ struct Args {
   float scale_log2;
   uint32_t flip;  // a negative scale negates the queries instead
 };
-
-// floor(y / d) for 0 <= y < 2^53 and 0 < d: the nearest quotient of two whole numbers does
-// not reach the next whole number.  (Some twenty instructions; a division of 64-bit
-// integers has over a hundred.)
-__device__ __forceinline__ int64_t whole(int64_t y, int64_t d) {
-  return (int64_t)floor((double)y / (double)d);
-}
 
 // Groups and lengths, from LDS where they fit.  The groups are valid only if their
 // bounds ascend from 0 to B.
@@ -149,58 +103,6 @@ struct Batch {
     return min(max(in_lds ? s_shared[g] : g_shared[g], 0), length(b));
   }
 };
-
-// An item of the line: the full chunks of a group's columns over its shared positions
-// (items 2 g), the other columns (2 g + 1), or a request's own positions.
-struct Item {
-  int request;     // the first one, whose table is read
-  int col0, cols;  // columns, counted from that request's first
-  int lo, hi;      // positions
-  int kind;
-  __device__ __forceinline__ int chunks() const {
-    return (cols - col0 + width_of(kind) - 1) >> width_log2(kind);
-  }
-  __device__ __forceinline__ int steps() const {
-    const int s = step_log2(kind);
-    return hi > lo ? ((hi - 1) >> s) - (lo >> s) + 1 : 0;
-  }
-  // cost of a unit but for its start
-  __device__ __forceinline__ int64_t work() const { return (int64_t)steps() * cost_of(kind); }
-};
-// Items of a kernel, and item i of them.
-template <int PART>
-__device__ __forceinline__ int items_of(const Args& a) {
-  return (PART == kOwn ? 0 : 2 * a.G) + (PART == kGroups ? 0 : a.B);
-}
-template <int D, int PART>
-__device__ __forceinline__ Item item_of(const Args& a, const Batch& batch, int i) {
-  Item t;
-  const int pairs = a.gq * a.sq;
-  if (PART == kGroups || (PART == kBoth && i < 2 * a.G)) {
-    constexpr int W = widest(D);
-    const int g = i >> 1;
-    t.request = batch.first(g);
-    const int cols = batch.valid ? (batch.first(g + 1) - t.request) * pairs : 0;
-    const int full = PART == kBoth ? 0 : cols & -W;
-    t.col0 = i & 1 ? full : 0;
-    t.cols = i & 1 ? cols : full;
-    t.kind = PART == kBoth ? rows_of(cols) : kind_of(D, i & 1 ? cols - full : W);
-    t.lo = 0, t.hi = t.cols > t.col0 ? batch.shared(g) : 0;
-  } else {
-    t.request = PART == kOwn ? i : i - 2 * a.G;
-    t.col0 = 0, t.cols = pairs;
-    t.lo = batch.valid ? batch.shared(batch.of(t.request)) : 0, t.hi = batch.length(t.request);
-    t.kind = a.own_kind;
-  }
-  return t;
-}
-
-// Where a chunk of `cols` columns from the request's `col` on has its place for a KV head
-// (counted in columns, one chunk after the other in the line's order): its entry of
-// `info`, and, with a gap of the widest chunk from each block to the next, its records.
-__device__ __forceinline__ int place_of(const Args& a, int request, int col, int cols, int kv) {
-  return (request * a.gq * a.sq + col) * a.Hkv + kv * cols;
-}
 
 // Where a block is on the line: at x, up to end; the window of items that is summed up
 // begins with item `window`.
@@ -239,16 +141,6 @@ struct Plan {
     return Batch{g.first, g.shared, g_lens, (Lds)first, (Lds)shared, (Lds)lens, g.G, g.max_pages * g.P,
                  g.G <= T && g.B <= 2 * T, valid};
   }
-  // An item's part of the line.
-  static __device__ __forceinline__ int64_t span(const Item& t) {
-    const int64_t work = t.work();
-    return work ? start_of(t.kind) + work : 0;
-  }
-  // Shares of a unit's work (below 2^31) of at most `most` each.
-  static __device__ __forceinline__ int shares(int work, float most) {
-    return work ? max((int)ceilf((float)work / most), 1) : 0;
-  }
-
   // All threads: the block's first segment; false: there is none.
   template <int D, int PART>
   __device__ __forceinline__ bool begin(const Args& g, const int32_t* g_lens) {
@@ -291,11 +183,10 @@ struct Plan {
     for (int w = 0; w < kTeams; ++w) work += sum[w], count += units[w], begins += starts[w];
     work = uniform(work), count = uniform(count), begins = uniform(begins);
     if (count == 0) return false;
-    constexpr int kLeast = cost_of(kRows1) * kRowWaves * kMinRows;
-    if (2 * count > blocks || n > T || work >= 0x40000000) {  // the line
+    if (takes_line(work, count, blocks, n, T)) {
       if (tid == 0) {
         a = g;
-        const int64_t piece = max(whole(work + begins, blocks) + 1, (int64_t)kLeast);
+        const int64_t piece = piece_of<D, PART>(work + begins, blocks);
         const int64_t from = blockIdx.x * piece;
         state = State{from, from, min(from + piece, work + begins), piece, -T, b.valid, false};
         upto[T] = 0;  // (no window yet)
@@ -304,11 +195,9 @@ struct Plan {
       return next<D, PART>(g_lens);
     }
 
-    // Shares: as many as there are blocks, or less.  Their length lies between work /
-    // blocks and work / (blocks - count); each wave counts those of one length, the
-    // least that are not too many are taken.
-    const float low = (float)work / (float)blocks, high = (float)work / (float)(blocks - count) * 1.0001f + 1.0f;
-    const float length = fmaxf(low + (high - low) * ((float)team / (kTeams - 1)), (float)kLeast);
+    // Shares: each wave counts those of one length, the least that are not too many are
+    // taken.
+    const float length = share_length(work, count, blocks, team, kTeams);
     __syncthreads();  // (`units` is written again)
     int many = 0;
     for (int i = lane; i < n; i += 64) {
@@ -339,27 +228,19 @@ struct Plan {
     for (int w = 0; w < kTeams; ++w) to += w < team ? starts[w] : 0;
     const int j = (int)blockIdx.x - (to - all);
     if (j >= 0 && j < all) {
-      const int u = (int)(((float)j + 0.5f) / (float)each), share = j - u * each;  // (both below 2^16)
-      const uint32_t steps = t.steps(), size = (steps + each - 1) / (uint32_t)each;
-      const int r0 = (int)min(share * size, steps), r1 = (int)min(r0 + size, steps);
-      put<D, PART>(g, t, tid, u, r0, r1, (int)((steps + size - 1) / size));
+      put<D, PART>(g, t, tid, cut_share(t, each, j));
     }
     __syncthreads();
     return uniform(segment.r0) < uniform(segment.r1);
   }
 
-  // Steps r0 .. r1 - 1 of unit u of item i, which leaves `records` records, the first of
-  // them by the block that has its first step.
+  // The block's segment of item i.
   template <int D, int PART>
-  __device__ __forceinline__ void put(const Args& g, const Item& it, int i, int u, int r0, int r1,
-                                      int records) {
-    const int chunk = (int)(((float)u + 0.5f) / (float)g.Hkv), kv = u - chunk * g.Hkv;  // (u below 2^17)
-    const int col = it.col0 + (chunk << width_log2(it.kind));
-    const int at = place_of(g, it.request, col, min(width_of(it.kind), it.cols - col), kv);
+  __device__ __forceinline__ void put(const Args& g, const Item& it, int i, const Cut& c) {
+    const Spot spot = spot_of(g, it, c.u);
     const bool own = PART == kOwn || (PART == kBoth && i >= 2 * g.G);
-    const int64_t rec = (int64_t)(own ? g.own_recs + g.own_gap * blockIdx.x : g.group_gap * blockIdx.x) + at;
-    if (r0 == 0 && r1 > 0) g.info[own ? g.own_info + at : at] = make_int2(blockIdx.x, records);
-    segment = Segment{it, col, kv, r0, r1, rec * (D + 4)};
+    if (c.r0 == 0 && c.r1 > 0) g.info[own ? g.own_info + spot.at : spot.at] = make_int2(blockIdx.x, c.records);
+    segment = Segment{it, spot.col, spot.kv, c.r0, c.r1, record_of(g, own, blockIdx.x, spot.at) * (D + 4)};
   }
 
   // All threads: the block's next segment; false: none is left.
@@ -380,7 +261,7 @@ struct Plan {
         if (window >= n) return false;
         const bool mine = window + tid < n;
         if (n > T && mine) items[tid] = item_of<D, PART>(a, batch(a, g_lens, state.valid), window + tid);
-        int64_t to = mine ? span(items[tid]) * (items[tid].chunks() * a.Hkv) : 0;
+        int64_t to = mine ? items[tid].span() * (items[tid].chunks() * a.Hkv) : 0;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
           const int64_t up = __shfl_up(to, o);
@@ -399,19 +280,9 @@ struct Plan {
       if (x >= upto[tid] && x < upto[tid + 1]) {  // one thread's item
         // the unit, and its steps that begin in the block's piece
         const Item it = items[tid];
-        const int cost = cost_of(it.kind), steps = it.steps();
-        const int64_t length = span(it), end = state.end, in = x - upto[tid], piece = state.piece;
-        const int u = in < length ? 0 : (int)whole(in, length);
-        const int64_t start = x - in + u * length, at = start + start_of(it.kind), work = it.work();
-        const int r0 = (int)whole(max(x - at, (int64_t)0) + cost - 1, cost);
-        int r1 = steps, more = 0;
-        if (end < at + work) {
-          r1 = (int)whole(max(end - at, (int64_t)0) + cost - 1, cost);
-          // the last step's piece, counted from this block's
-          more = (int)whole(at + work - cost - state.begin, piece);
-        }
-        put<D, PART>(a, it, window + tid, u, r0, r1, 1 + more);
-        state.x = start + length;
+        const Cut c = cut_line(it, upto[tid], x, state.begin, state.end, state.piece);
+        put<D, PART>(a, it, window + tid, c);
+        state.x = c.next;
       }
       __syncthreads();
       if (uniform(segment.r0) < uniform(segment.r1)) return true;  // (else a unit's start alone)
@@ -870,9 +741,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   Batch batch{a.first, a.shared, lens, nullptr, nullptr, nullptr, a.G, a.max_pages * a.P, false, true};
   const int i = blockIdx.x * 64 + lane, pair = min(i / (D / 4), pairs - 1), d4 = i % (D / 4);
   // what does not wait for the groups: the request's own records
-  const int own_width = width_of(a.own_kind), own_col = pair & -own_width;
-  const int own_at = place_of(a, b, own_col, min(own_width, pairs - own_col), kv);
-  const int2 own = a.info[a.own_info + own_at];  // (nothing of use where it has none)
+  const Asked mine = own_of(a, b, pair, kv);
+  const int2 own = a.info[a.own_info + mine.at];  // (nothing of use where it has none)
   const int len = batch.length(b);
   int group, from, to, shared;  // the request's group, its requests and shared positions
   if (a.G < 64) {       // a lane for each bound: two loads in a row less (16 requests over 8,192 positions 23.8 -> 23.5 us)
@@ -923,18 +793,12 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
     }
   };
   if (shared > 0) {
-    constexpr int W = widest(D);
-    const int cols = (to - from) * pairs;
-    const int col = (b - from) * pairs + pair, full = both ? 0 : cols & -W;
-    const int begin = col < full ? 0 : full, end = col < full ? full : cols;
-    const int width = width_of(both ? rows_of(cols) : kind_of(D, col < full ? W : cols - full));
-    const int first = begin + ((col - begin) & -width);  // of its chunk
-    const int at = place_of(a, from, first, min(width, end - first), kv);
-    const int2 in = a.info[at];
-    add(at + in.x * a.group_gap + col - first, a.group_gap, min(in.y, group_blocks));
+    const Asked ours = group_of<D>(a, both, from, to, b, pair, kv);
+    const int2 in = a.info[ours.at];
+    add(ours.at + in.x * a.group_gap + ours.in, a.group_gap, min(in.y, group_blocks));
   }
   if (len > shared)
-    add(a.own_recs + own_at + own.x * a.own_gap + pair - own_col, a.own_gap, min(own.y, own_blocks));
+    add(a.own_recs + mine.at + own.x * a.own_gap + mine.in, a.own_gap, min(own.y, own_blocks));
   s_num[wave][lane] = num;
   s_ml[wave][lane] = f32x2{M, den};
   __syncthreads();
@@ -955,42 +819,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void kv8_shared_join_kernel(
   *reinterpret_cast<uint2*>(out + row * D + 4 * d4) =
       make_uint2(narrow2<BF16>(num.x * r, num.y * r), narrow2<BF16>(num.z * r, num.w * r));
   if (lse && d4 == 0) lse[row] = den > 0.0f ? (mx + __log2f(den)) * kLn2 : -INFINITY;
-}
-
-// How the workspace is laid out: entries, then records.
-struct Layout {
-  bool both;  // one kernel for groups and requests
-  int group_blocks, own_blocks, own_kind, group_gap, own_gap, own_info, own_recs;
-  size_t recs, bytes;
-};
-Layout layout_of(const jf_kv_layout& L, int32_t B, int32_t sq, int32_t Hq, bool both) {
-  const int D = L.head_dim, pairs = Hq / L.num_kv_heads * sq, columns = B * Hq * sq;
-  Layout p;
-  p.both = both;
-  p.own_kind = rows_of(pairs);
-  p.own_blocks = row_blocks(D, !both && p.own_kind == kRows1) * num_cus();
-  p.group_blocks = both ? p.own_blocks : num_cus();
-  p.group_gap = both ? width_of(kRows2) : widest(D);
-  p.own_gap = std::min(pairs, width_of(p.own_kind));
-  p.own_info = columns;
-  p.own_recs = columns + p.group_blocks * p.group_gap;
-  p.recs = ((size_t)columns * 2 * sizeof(int2) + 15) / 16 * 16;
-  p.bytes = p.recs + (size_t)(p.own_recs + columns + p.own_blocks * p.own_gap) * (D + 4) * sizeof(float);
-  return p;
-}
-// Whether rows are walked for groups too, in one kernel with the requests' own positions:
-// for batches of up to 128 columns (rows against tiles, 32/8 heads of 128, 32 requests:
-// over 65,536 positions 70 against 80 us, over 4,096 and 300 of their own 29 against 42;
-// 24/4 heads of 256, 21 requests over 32,768: 53 against 55), and for more where columns,
-// heads and the table's positions are too few to pay for a kernel of tiles, whose records
-// are wider and whose start is longer (64 requests over 4,096: 37 against 58 us, over
-// 16,384: 70 both, over 32,768: 107 against 87; 256 over 4,096: 93 against 96, over 8,192:
-// 135 against 113; heads of 256, 42 requests: over 4,096 35 against 50, over 16,384 62
-// both, over 32,768 97 against 79).
-bool by_rows(const jf_kv_layout& L, int32_t B, int32_t sq, int32_t Hq, int32_t max_pages) {
-  const int64_t columns = (int64_t)B * (Hq / L.num_kv_heads) * sq;
-  const int64_t few = L.head_dim > 128 ? 1 << 24 : 1 << 25;
-  return columns <= 128 || columns * L.num_kv_heads * ((int64_t)max_pages * L.page_size) <= few;
 }
 
 template <int D, bool BF16>
@@ -1029,7 +857,7 @@ hipError_t launch_t(const Cache& in, const int32_t* lens, const Args& a, const L
 }  // namespace
 
 size_t kv8_shared_bytes(const jf_kv_layout& L, int32_t B, int32_t, int32_t sq, int32_t Hq) {
-  return std::max(layout_of(L, B, sq, Hq, true).bytes, layout_of(L, B, sq, Hq, false).bytes);
+  return std::max(layout_of(L, B, sq, Hq, true, num_cus()).bytes, layout_of(L, B, sq, Hq, false, num_cus()).bytes);
 }
 
 hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
@@ -1038,7 +866,7 @@ hipError_t launch_kv8_shared(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
                              const int32_t* group_start, const int32_t* shared_lens, int32_t G,
                              float softmax_scale, void* ws, void* out, float* lse,
                              hipStream_t stream) {
-  const Layout p = layout_of(L, B, sq, Hq, by_rows(L, B, sq, Hq, max_pages));
+  const Layout p = layout_of(L, B, sq, Hq, by_rows(L, B, sq, Hq, max_pages), num_cus());
   int shift = 0;
   while ((1 << shift) < L.group_size) ++shift;
   const Cache in{static_cast<const uint8_t*>(pool.k_codes), static_cast<const uint8_t*>(pool.k_meta),
