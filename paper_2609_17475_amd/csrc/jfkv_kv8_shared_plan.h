@@ -52,7 +52,14 @@ __host__ __device__ constexpr int cost_of(int kind) {
   return kind == kRows1 ? 4 : kind == kRows2 ? 5 : kind == kTiles1 ? 16 : 24;
 }
 __host__ __device__ constexpr int start_of(int kind) { return kind >= kTiles1 ? 60 : 30; }
-// The least that a piece of the line, or a share of a unit, costs.
+// The dearest step of a kernel's units.
+__host__ __device__ constexpr int dearest_step(int D, int part) {
+  return cost_of(part == kGroups ? kind_of(D, widest(D)) : kRows2);
+}
+static_assert(cost_of(kRows1) <= cost_of(kRows2) && cost_of(kRows2) <= cost_of(kTiles1) &&
+                  cost_of(kTiles1) <= cost_of(kTiles2),
+              "dearest_step takes the widest kind for the dearest");
+// The least that a share of a unit costs, or a piece of the line for its length.
 constexpr int kLeast = cost_of(kRows1) * kRowWaves * kMinRows;
 
 // Blocks of the row walk per CU.  One set of columns leaves room for more, which hides
@@ -136,10 +143,13 @@ struct Cut {
 };
 
 // The line: the units follow one another, each with its start's cost, and the line is cut
-// into pieces of one length, a block each.
+// into pieces of one length, a block each.  No piece is shorter than a step of any unit:
+// between the blocks of a unit's first and last step each then has the beginning of a
+// step, and so a record, as cut_line counts them.
 template <int D, int PART>
 JF_PLAN int64_t piece_of(int64_t line, int blocks) {
-  return std::max(whole(line, blocks) + 1, (int64_t)kLeast);
+  constexpr int least = std::max(kLeast, dearest_step(D, PART));
+  return std::max(whole(line, blocks) + 1, (int64_t)least);
 }
 // The unit of item `it` (which begins at `from`) that place x lies in, and its steps that
 // begin in begin .. end - 1, a block's piece of the line that holds x.
@@ -155,7 +165,7 @@ JF_PLAN Cut cut_line(const Item& it, int64_t from, int64_t x, const int64_t& beg
   int r1 = steps, more = 0;
   if (end < at + work) {
     r1 = upto(end);
-    // the last step's piece, counted from this block's
+    // the last step's piece, counted from this block's (each between has a step)
     more = (int)whole(at + work - cost - begin, piece);
   }
   return {u, r0, r1, 1 + more, start + length};
