@@ -807,10 +807,15 @@ typedef enum { JF_ROPE_HALVES = 0, JF_ROPE_PAIRS = 1 } jf_rope_order;
  *                    fastest pair stays, the slowest is divided by factor
  *   JF_ROPE_PARTS    pairs of more than `fast` turns in original_len positions stay,
  *                    those of fewer than `slow` are divided by factor, between them
- *                    lies a ramp over the pairs' numbers ("YaRN", arXiv 2309.00071):
+ *                    lies a ramp over the pairs' numbers:
  *                    i(r) = rot_dim ln(original_len / (2 pi r)) / (2 ln base), the ramp
  *                    from floor(i(fast)), at least 0, to ceil(i(slow)), at most
- *                    rot_dim - 1; m = 0.1 ln(factor) + 1 (factor <= 1: 1) */
+ *                    rot_dim - 1 (without length where all pairs lie on one side of
+ *                    it: they stay, or from ceil(i(slow)) on are divided);
+ *                    m = 0.1 ln(factor) + 1 (factor <= 1: 1).  The parts and the
+ *                    magnitude are those of "YaRN" (arXiv 2309.00071), whose own ramp
+ *                    is linear in a pair's turns, and not in its number as it is here
+ *                    and in models that are published with this scaling */
 typedef enum {
   JF_ROPE_PLAIN = 0,
   JF_ROPE_LINEAR = 1,

@@ -97,7 +97,8 @@ jf_status jf_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, dou
     double slowed = 0.0;  // the share that is divided by factor
     if (scaling == JF_ROPE_LINEAR) slowed = 1.0;
     if (scaling == JF_ROPE_PARTS)
-      slowed = hi > lo ? std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0) : (i > lo ? 1.0 : 0.0);
+      // (no ramp where all pairs lie on one side of it: behind its end, they are divided)
+      slowed = hi > lo ? std::min(std::max((i - lo) / (hi - lo), 0.0), 1.0) : (i >= hi ? 1.0 : 0.0);
     inv_freq[i] = (float)(slowed > 0.0 ? f * (1.0 - slowed) + f / factor * slowed : f);
   }
   return ok();
