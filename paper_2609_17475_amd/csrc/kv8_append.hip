@@ -23,6 +23,7 @@
 
 #include "jfkv_internal.h"
 #include "jfkv_kv8.h"
+#include "jfkv_kv8_append_grid.h"
 #include "jfkv_rope.h"
 
 namespace jfkv {
@@ -66,13 +67,6 @@ struct Turn {
 };
 struct NoTurn {};
 
-// A table that outgrows an XCD's L2 (4 MB) is read by all heads and parts of a block of
-// tokens one after the other on one XCD: 65,535 rows, 34 MB of angles, 327 -> 318 us, 848
-// MB read for 1,133.  (Few blocks would be shared out unevenly: 2,048 rows, 0.5 MB, take
-// 15.4 us in the grid's order, 15.0 to 16.9 with a block's heads on one XCD.)
-constexpr uint32_t kXcds = 8;
-constexpr int64_t kTableTogether = 4 << 20;
-
 // 8 dims of a row of head_dim D, from dim `base` on, rotated; the partner dims are
 // read from the row as well (they are another lane's, in the first-level cache).  65,535
 // rows of 8 heads of 128 and 32 of queries: 313-319 us, 4.7-4.8 TB/s in and out of HBM; a row of
@@ -109,18 +103,14 @@ __device__ __forceinline__ void turn8(uint32_t (&raw)[4], const uint16_t* x, con
   }
 }
 
-// The rows of queries, a token's heads by a block at a time: together, a unit takes a run
-// of tokens and block h of its `heads` every `heads`-th of them; else all blocks take
-// turns.
+// The rows of queries, a token's heads by a block at a time.
 template <bool BF16, bool PAIRS>
 __device__ __forceinline__ void turn_queries(const Turn& r, int D, int unit, int units, int h, int heads,
                                              int total) {
   using namespace rope;
   const int items = D / 16, n_rot = r.half / 8;
-  const int64_t run = (total + (int64_t)units - 1) / units;
-  const int64_t end = r.together ? min((unit + 1) * run, (int64_t)total) : total;
-  const int64_t step = r.together ? heads : (int64_t)heads * units;
-  for (int64_t t = r.together ? unit * run + h : h * (int64_t)units + unit; t < end; t += step) {
+  const append::Tokens turn_of = append::tokens_of(r.together, unit, units, h, heads, total);
+  for (int64_t t = turn_of.first; t < turn_of.end; t += turn_of.step) {
     const float* const angles = r.table + row_of(r.rows, r.table_rows, t) * (2 * (int64_t)r.half);
     for (int i = threadIdx.x; i < r.q_heads * items; i += blockDim.x) {
       const int item = i % items, at = i / items * D;
@@ -161,10 +151,8 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(
   const int64_t cap = (int64_t)max_pages * P;
   if constexpr (ROPE) {
     if (rope.together) {
-      const uint32_t parts = gridDim.y * gridDim.z;
-      const uint32_t at = unit + gridDim.x * (h + gridDim.y * part), slot = at / kXcds;
-      unit = slot / parts * kXcds + at % kXcds;
-      h = slot % parts % gridDim.y, part = slot % parts / gridDim.y;
+      const append::Place at = append::place_of(unit, h, part, gridDim.x, gridDim.y, gridDim.z);
+      unit = at.unit, h = at.head, part = at.part;
     }
     if (part == 2) {
       if (rope.pairs)
@@ -344,15 +332,10 @@ template <bool ROPE, class T>
 hipError_t launch_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
                          const void* k_new, const void* v_new, const int32_t* cu_tok,
                          const int32_t* start_pos, const int32_t* block_tables, int32_t B,
-                         int32_t max_pages, int32_t total_tok, const T& rope, int parts,
+                         int32_t max_pages, int32_t total_tok, const T& rope, int64_t units, int parts,
                          hipStream_t stream) {
   const int block = L.group_size, items = block * L.head_dim / 16;
   const int threads = std::min(items, 256);
-  // blocks that total_tok rows of B requests can touch: one per row at most,
-  // and whole blocks plus two partial ones per request
-  int64_t units = std::min<int64_t>(total_tok, total_tok / block + 2 * (int64_t)B);
-  if constexpr (ROPE)
-    if (rope.together) units = (units + kXcds - 1) / kXcds * kXcds;
   const dim3 grid((uint32_t)units, L.num_kv_heads, parts);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, static_cast<uint8_t*>(pool.k_codes),
@@ -377,7 +360,8 @@ hipError_t launch_kv8_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool,
                              const int32_t* start_pos, const int32_t* block_tables, int32_t B,
                              int32_t max_pages, int32_t total_tok, hipStream_t stream) {
   return launch_append<false>(L, pool, bf16, k_new, v_new, cu_tok, start_pos, block_tables, B,
-                              max_pages, total_tok, NoTurn{}, 2, stream);
+                              max_pages, total_tok, NoTurn{}, append::units_of(total_tok, B, L.group_size), 2,
+                              stream);
 }
 
 hipError_t launch_kv8_rope_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& pool, bool bf16,
@@ -386,11 +370,13 @@ hipError_t launch_kv8_rope_append(const jf_kv_layout& L, const jf_kv_pool_ptrs& 
                                   void* q_out, int32_t Hq, const int32_t* cu_tok,
                                   const int32_t* start_pos, const int32_t* block_tables, int32_t B,
                                   int32_t max_pages, int32_t total_tok, hipStream_t stream) {
+  const int parts = q ? 3 : 2;
+  const append::Grid grid = append::grid_of(total_tok, B, L.group_size, r.rot_dim, L.num_kv_heads, parts);
   const Turn turn{r.table, r.rows, r.table_rows, r.rot_dim / 2, r.order == JF_ROPE_PAIRS,
                   k_stride, v_stride, q_stride, static_cast<const uint16_t*>(q),
-                  static_cast<uint16_t*>(q_out), Hq, (int64_t)total_tok * r.rot_dim * 4 > kTableTogether};
+                  static_cast<uint16_t*>(q_out), Hq, grid.together};
   return launch_append<true>(L, pool, bf16, k_new, v_new, cu_tok, start_pos, block_tables, B,
-                             max_pages, total_tok, turn, q ? 3 : 2, stream);
+                             max_pages, total_tok, turn, grid.units, parts, stream);
 }
 
 }  // namespace jfkv
