@@ -5,6 +5,8 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2609_17475_amd import jfkv
+from tests.kv8_cases import i32, rows
 from tests.test_gpu_kv8_shared import Batch
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +69,52 @@ def test_long_lines_of_tiles(hkv, gq, d, sq, sizes, shared):
     b = Batch(rng, 64, hkv, hkv * gq, d, 64, d == 128, sizes, shared, lens, sq)
     ends = np.cumsum([0] + sizes).tolist()
     run(b, sorted({i for lo, hi in zip(ends, ends[1:]) for i in (lo, lo + 1, (lo + hi) // 2, hi - 1)}))
+
+
+@pytest.mark.parametrize("d,bf16", [(128, False), (256, True)])
+def test_captured_with_other_groups(d, bf16):
+    """A captured call over wide tables, replayed with groups, lengths and queries that put
+    its units on a line or not, with the same call on another stream beside it."""
+    rng = np.random.default_rng(d)
+    B, G, hkv, hq = 100, 40, 8, 32
+    lens = [int(x) for x in rng.integers(260, 400, B)]
+    b = Batch(rng, 64, hkv, hq, d, 16, bf16, [1] * B, [0] * B, lens, 1)
+    b.tables[1:, :4] = b.tables[0, :4]  # 256 positions that all of them share
+    tables = np.full((B, 2 ** 25 // (B * hq * 64) + 1), -1, np.int32)
+    tables[:, :b.tables.shape[1]] = b.tables
+    b.tables = tables
+    groups = [
+        ([0] + [B] * G, [256] + [0] * (G - 1)),                                   # one of all
+        (list(range(0, 2 * G, 2)) + [B], [int(x) for x in rng.integers(1, 257, G)]),  # pairs, and one of 22
+        (list(range(G)) + [B], [0] * (G - 1) + [200]),                            # alone, and one of 61
+        ([0, 50] + [B] * (G - 1), [130, 256] + [7] * (G - 2)),
+    ]
+    n = jfkv.jf_kv8_shared_workspace_bytes(b.p.lay, B, G, 1, hq)
+    w1, w2 = (torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(2))
+    q = b.q.cuda()
+    out, out2, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(B, 1, hq, device="cuda")
+    lens_d, first, shared = i32(lens), i32(groups[0][0]), i32(groups[0][1])
+    call = [b.p.gpu, q, i32(tables), lens_d, first, shared, b.scale]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        jfkv.jf_kv8_shared_attn(*call, w1, out, lse=lse)
+    side = torch.cuda.Stream()
+    for turn, (bounds, most) in enumerate(groups + groups[:2]):
+        b.first, b.shared = bounds, most
+        b.lens = [0 if x < 10 else int(rng.integers(257, m + 1)) for x, m in zip(rng.integers(0, 100, B), lens)]
+        for lo in bounds[:-1]:
+            if lo < B:
+                b.lens[lo] = lens[lo]  # (whose table is read)
+        b.lead = np.repeat(bounds[:-1], np.diff(bounds))
+        wide = np.repeat(np.where(np.diff(bounds) > 1, most, 0), np.diff(bounds))
+        b.cut = [int(x) for x in wide]
+        b.q = rows(rng, B, hq, d, bf16, 0.7).view(B, 1, hq, d)
+        for to, new in ((q, b.q), (lens_d, i32(b.lens)), (first, i32(bounds)), (shared, i32(most))):
+            to.copy_(new)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            jfkv.jf_kv8_shared_attn(*call, w2, out2)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, out2)
+        b.check(out, lse, only=sorted(set(range(turn, B, 9)) | {0, B - 1}))
