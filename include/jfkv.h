@@ -752,8 +752,10 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
                        float* kept_weights, hipStream_t stream);
 
 /* Decode attention of a batch whose requests share prefixes: as jf_kv8_decode_attn
- * (the same queries, masks, types and limits), with the positions that a group's
- * requests have in common read once for all of them.
+ * (the same queries, masks, types, roundings and limits), with the positions that a
+ * group's requests have in common read once for all of them.  Attention weights are not
+ * added up here: a program that evicts by them takes them from jf_kv8_decode_attn or
+ * jf_kv8_attn_weights.
  *   group_start  int32 [num_groups + 1] (device): requests group_start[g] ..
  *                group_start[g + 1] - 1 are group g; ascending from 0 to B (otherwise
  *                every request is computed by itself).  Groups of one request, or none,
@@ -771,7 +773,9 @@ jf_status jf_kv8_evict(const jf_kv_layout* layout, const jf_kv_pool_ptrs* pool,
  *                logarithm of the sum of exp(softmax_scale * q . k) over the positions
  *                seen (-inf where there is none, for which out is zero)
  * Lengths and groups are read on the device: a captured call can be replayed with
- * others.  Two calls with the same inputs give the same bits; a request's results in
+ * others.  The kernels are chosen on the host by B, the heads and max_pages, an upper
+ * bound of what is read: tables far wider than the requests are long cost time (64
+ * requests over 4,096 positions, 32/8 heads of 128: 37 us, or 58).  Two calls with the same inputs give the same bits; a request's results in
  * another batch are the same up to the order of sums.  B <= 65,535,
  * B * num_q_heads * num_queries <= 65,536, 1 <= num_groups <= B. */
 jf_status jf_kv8_shared_workspace_bytes(const jf_kv_layout* layout, int32_t B,
@@ -862,7 +866,7 @@ typedef struct {
  *          input (same pointer and stride); otherwise the memory of outputs must not
  *          overlap that of inputs or of the other output.
  * head_dim even and at most 65536, rot_dim <= head_dim, strides at least heads *
- * head_dim where total_tok > 1.  Addresses aligned to an element are enough; 16 bytes,
+ * head_dim where total_tok > 1 and at most 2^31.  Addresses aligned to an element are enough; 16 bytes,
  * with sizes and strides of multiples of 16 and 8 elements, are fastest. */
 jf_status jf_rope_rotate(const jf_rope* rope, int32_t dtype, int32_t head_dim, int32_t transpose,
                          const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
@@ -876,7 +880,7 @@ jf_status jf_rope_rotate(const jf_rope* rope, int32_t dtype, int32_t head_dim, i
  *   rope      as above, rot_dim a multiple of 16 and at most the layout's head_dim
  *   k_new, v_new  [total_tok][Hkv][d] (device, 16-byte aligned), k_stride and
  *             v_stride elements from one token to the next (multiples of 8, at least
- *             Hkv * d where total_tok > 1)
+ *             Hkv * d where total_tok > 1, at most 2^31)
  *   q, q_out  NULL, or [total_tok][num_q_heads][d] (device, 16-byte aligned), q with
  *             q_stride as above, q_out without gaps; q_out may be q where q has none
  * The positions that turn a key need not be the cache's (after an eviction they are

@@ -141,6 +141,7 @@ struct Plan {
     return Batch{g.first, g.shared, g_lens, (Lds)first, (Lds)shared, (Lds)lens, g.G, g.max_pages * g.P,
                  g.G <= T && g.B <= 2 * T, valid};
   }
+
   // All threads: the block's first segment; false: there is none.
   template <int D, int PART>
   __device__ __forceinline__ bool begin(const Args& g, const int32_t* g_lens) {
@@ -227,9 +228,7 @@ struct Plan {
 #pragma unroll
     for (int w = 0; w < kTeams; ++w) to += w < team ? starts[w] : 0;
     const int j = (int)blockIdx.x - (to - all);
-    if (j >= 0 && j < all) {
-      put<D, PART>(g, t, tid, cut_share(t, each, j));
-    }
+    if (j >= 0 && j < all) put<D, PART>(g, t, tid, cut_share(t, each, j));
     __syncthreads();
     return uniform(segment.r0) < uniform(segment.r1);
   }
